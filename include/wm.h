@@ -417,6 +417,132 @@ wm_status wm_decode_verify_opt(const void* wire, uint64_t wire_len, void* dst, c
 wm_status wm_checksum_noalloc(const void* cache, uint64_t nbytes, uint32_t chunk_bytes,
                               uint32_t* crc_out, void* stream);
 
+/*
+ * Paged 8-bit cache - the attention cache as a serving engine fills and reads it between two moves.
+ * Paper: the movable state is the attention cache of a running session (Section 3.1); the text-model
+ * session of the model-blind move (Section 5) holds an append-only cache of which each step writes
+ * one token.  The paper stops at the bytes; these calls are what a session does with them before it leaves
+ * and after it has arrived.  A moved session goes on bit for bit: pages are ordinary device memory and
+ * can be leaves of wm_encode_leaves, and the outputs depend on the pages' contents, not on their numbers.
+ *
+ * A pool has n_pages pages of page_tokens tokens.  Keys and values are e4m3 codes; one f32 scale
+ * for every page and head (for keys and for values) gives value = code * scale.
+ */
+typedef struct {
+    void*    k;             /* [dev] e4m3 codes; token t, head h, page p, channel d at k + p * page_stride + h * head_stride + t * token_stride + d */
+    void*    v;             /* [dev] the same for values, same strides */
+    float*   k_scale;       /* [dev] f32[n_pages * kv_heads], finite and not negative */
+    float*   v_scale;       /* [dev] */
+    uint64_t page_stride;   /* bytes; multiples of 16, the three in any order; no two elements share a byte */
+    uint64_t head_stride;
+    uint64_t token_stride;
+    uint32_t n_pages;       /* 1 .. ; n_pages * page_tokens < 2^31 */
+    uint32_t page_tokens;   /* 16, 32, 64 or 128 */
+    uint32_t kv_heads;      /* 1 .. 1024 */
+    uint32_t head_dim;      /* 64 or 128 */
+} wm_pages;
+
+/* What went wrong on the device in the pages calls.  The calls write it only when they find a fault,
+ * so one record (zeroed by the caller) can stand over a whole step of many calls.  16 bytes. */
+typedef struct {
+    int32_t  status;        /* 0, or the lowest wm_status found                          */
+    uint32_t first;         /* 1 + the lowest index concerned (a request, or a row of the append); 0: none */
+    uint32_t reserved[2];
+} wm_pages_report;
+
+/* Rows of heads: element d of head h of row r at ptr + r * row_stride + h * head_stride + d (strides in
+ * elements, their bytes multiples of 16; ptr 16-byte aligned). */
+typedef struct {
+    void*    ptr;           /* [dev] */
+    uint64_t row_stride;
+    uint64_t head_stride;
+} wm_rows;
+
+#define WM_TYPE_BF16 0
+#define WM_TYPE_F16 1
+#define WM_TYPE_F32 2      /* wm_pages_append's input only */
+#define WM_PAGES_MAX_REQUESTS 4000u
+
+/*
+ * wm_pages_plan - block tables and slot map of one step from the requests' lengths.
+ * Request i had old_len[i] tokens and has new_len[i] after the step.  With held = ceil(old / page_tokens) and
+ * want = ceil(new / page_tokens):
+ *   - a request that shrinks (0: it has ended) gives its pages [want, held) back: in request order, page
+ *     order inside a request, they are written behind the *free_count pages of the free list;
+ *   - a request that grows takes want - held pages, in the same order, from the end of the list (pages given
+ *     back in this very call included, the last one first) into its row of the table;
+ *   - start[i] = tokens appended by the requests before i (n_requests + 1 entries), and slots[start[i] + j] =
+ *     page * page_tokens + offset of position old_len[i] + j; slots behind the last token get -1.
+ * Entries of the table that no request takes, and of the free list at or behind *free_count_out, are left as they are
+ * (but those a request gives back and no request takes, which are written).  The call is made for replay in
+ * a graph: free_count_out may be free_count.  It is the same for every input order of the free list.
+ *   old_len, new_len  [dev] i32[n_requests], 1 .. WM_PAGES_MAX_REQUESTS requests
+ *   table      [dev] i32[n_requests][table_stride]: pages of each request in order; n_requests * table_stride < 2^31
+ *   free_pages [dev] i32[n_pages]
+ *   free_count, free_count_out [dev] u32
+ *   start      [dev] i32[n_requests + 1]
+ *   slots      [dev] i32[n_slots]
+ *   report     [dev] or NULL.  WM_ERR_ARG: a length below zero, more pages held than the row has, a free count that
+ *              does not fit the pool.  WM_ERR_CAPACITY: a length beyond the row of the table, not enough free pages, more
+ *              tokens than slots.  Then nothing is taken or given: the table and the list stay, *free_count_out =
+ *              *free_count, start is all 0 and slots all -1, so that the calls behind it do nothing.  A page number
+ *              outside the pool (WM_ERR_ARG) makes the slots of that page's tokens -1.
+ */
+wm_status wm_pages_plan(const int32_t* old_len, const int32_t* new_len, uint32_t n_requests, uint32_t page_tokens, uint32_t n_pages,
+                        int32_t* table, uint32_t table_stride, int32_t* free_pages, const uint32_t* free_count,
+                        uint32_t* free_count_out, int32_t* start, int32_t* slots, uint32_t n_slots,
+                        wm_pages_report* report, void* stream);
+
+/*
+ * wm_pages_append - keys and values of a step's new tokens into the pool, in 8 bits.
+ * Row r goes to slot slots[r] (page * page_tokens + offset); a row whose slot is -1 is left out.  Rows of one page
+ * stand one behind the other with ascending offsets, as wm_pages_plan lists them; the lowest offset says
+ * how many tokens of the page (those before it) are kept.  Per page and head, for keys and values alike:
+ *   need  = the smallest power of two with amax <= 448 * need (amax over the new rows' finite values; not below 2^-126)
+ *   scale = need where no token is kept, else the larger of need and the power of two that is not below the old scale
+ *   kept codes become round(code * old scale / scale), new ones round(x / scale), to the nearest e4m3 value,
+ *   ties to even; infinities become +-448, NaN stays NaN.
+ * A power of two as scale costs at most one step of e4m3's range and nothing of its precision, and growing a
+ * scale is exact for every code that stays normal.
+ *   k, v    rows of kv_heads heads of the pool's head_dim, n_rows of them, of type WM_TYPE_*
+ *   slots   [dev] i32[n_rows]
+ *   report  [dev] or NULL: WM_ERR_ARG with the lowest row concerned where a slot is neither -1 nor in the pool, or
+ *           is in its predecessor's page without being its successor; those rows are left out.
+ * No page may be written through two runs of rows of one call (two requests that append to the same page): its
+ * contents are then unspecified, other pages are as they should be.
+ */
+wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows* v, int type, const int32_t* slots, uint32_t n_rows,
+                          wm_pages_report* report, void* stream);
+
+/*
+ * wm_pages_attend - attention of a step's queries over the pool.
+ * Request i has rows q_start[i] .. q_start[i + 1] - 1 of q, which stand at its last positions: row j of n at position
+ * kv_len[i] - n + j.  Query head h reads key head h / (q_heads / kv_heads).  A row at position p sees the request's tokens
+ * t < kv_len[i], with causal only t <= p, with a window of w > 0 (causal only) only t > p - w.
+ *   out = sum_t softmax_t(scale * q . key_t) value_t,   lse = log sum_t exp(scale * q . key_t)
+ * A row that sees nothing (a position below zero, no tokens) gets zeros and -infinity.  Rows behind the last request's are
+ * left as they are.  Codes a row does not see do not touch it, whatever they hold (NaN included).
+ *   table     [dev] i32[n_requests][table_stride], kv_len [dev] i32[n_requests], q_start [dev] i32[n_requests + 1]
+ *   q, out    n_rows rows of q_heads heads of the pool's head_dim, WM_TYPE_BF16 or WM_TYPE_F16; must not overlap
+ *   lse       [dev] f32[n_rows][q_heads] or NULL
+ *   q_heads   a multiple of kv_heads, at most 64 * kv_heads
+ *   max_q     the most rows any request has, as far as the caller knows (1: a step of single tokens).  It
+ *             chooses the kernels; requests with more rows are answered all the same, more slowly
+ *   options   WM_ATTEND_CAUSAL or 0
+ *   workspace [dev] wm_pages_workspace_bytes(head_dim) bytes, 16-byte aligned, contents arbitrary
+ *   report    [dev] or NULL.  WM_ERR_ARG with the lowest request concerned: a negative length, a length beyond its row of
+ *             the table, row numbers that decrease or lie outside 0 .. n_rows (its rows are left as they are), or
+ *             a page number outside the pool (rows that see it get NaN).  WM_ERR_TIMEOUT: a wait ran out (see
+ *             wm_wait_budget_ms); outputs that are not there are NaN
+ * Sums and softmax statistics are held in 32 bits.  The result of a row does not depend on the other requests' contents.
+ */
+#define WM_ATTEND_CAUSAL 1u
+uint64_t wm_pages_workspace_bytes(uint32_t head_dim);
+wm_status wm_pages_attend(const wm_pages* pages, const int32_t* table, uint32_t table_stride, const int32_t* kv_len,
+                          const int32_t* q_start, uint32_t n_requests, const wm_rows* q, const wm_rows* out, int type, float* lse,
+                          uint32_t n_rows, uint32_t q_heads, uint32_t max_q, float scale, uint32_t options, uint32_t window,
+                          void* workspace, uint64_t workspace_bytes, wm_pages_report* report, void* stream);
+
 /* Number of kernels the last call on this host thread enqueued (for launch accounting). */
 uint32_t wm_last_launch_count(void);
 

@@ -26,7 +26,7 @@ EXPORTS = ("wm_num_chunks", "wm_num_tiles", "wm_meta_bytes", "wm_wire_bound", "w
            "wm_timing_enable", "wm_timing_read_ms", "wm_checksum_noalloc", "wm_encode_leaves",
            "wm_decode_verify_leaves", "wm_zero_tiles_enable", "wm_decode_verify_strict", "wm_checksum_poly", "wm_entropy_enable",
            "wm_encode_opt", "wm_decode_verify_opt", "wm_checksum_xxh64", "wm_wait_budget_ms", "wm_workspace_status",
-           "wm_inject_stall")
+           "wm_inject_stall", "wm_pages_plan", "wm_pages_append", "wm_pages_workspace_bytes", "wm_pages_attend")
 
 
 class WmError(RuntimeError):
@@ -86,6 +86,15 @@ def load_library() -> ctypes.CDLL:
     lib.wm_encode_leaves.argtypes = [vp, u32, u64, u32, vp, vp, vp, u64, vp, u64, vp, vp]
     lib.wm_decode_verify_leaves.restype = ctypes.c_int
     lib.wm_decode_verify_leaves.argtypes = [vp, u64, vp, u32, u64, u32, vp, vp, u64, vp, vp]
+    lib.wm_pages_workspace_bytes.restype = u64
+    lib.wm_pages_workspace_bytes.argtypes = [u32]
+    lib.wm_pages_plan.restype = ctypes.c_int
+    lib.wm_pages_plan.argtypes = [vp, vp, u32, u32, u32, vp, u32, vp, vp, vp, vp, vp, u32, vp, vp]
+    lib.wm_pages_append.restype = ctypes.c_int
+    lib.wm_pages_append.argtypes = [vp, vp, vp, ctypes.c_int, vp, u32, vp, vp]
+    lib.wm_pages_attend.restype = ctypes.c_int
+    lib.wm_pages_attend.argtypes = [vp, vp, u32, vp, vp, u32, vp, vp, ctypes.c_int, vp, u32, u32, u32, ctypes.c_float, u32, u32,
+                                    vp, u64, vp, vp]
     return lib
 
 
@@ -391,3 +400,142 @@ def wm_decode_verify_leaves(wire: torch.Tensor, wire_len: int, leaf_table: torch
                                          int(nbytes), chunk_bytes, dst_crc_inout.data_ptr(), workspace.data_ptr(),
                                          workspace.numel(), result.data_ptr(), _stream(stream)),
            "wm_decode_verify_leaves")
+
+
+# ---------------------------------------------------------------- the paged 8-bit cache
+
+class _CPages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("page_stride", ctypes.c_uint64), ("head_stride", ctypes.c_uint64), ("token_stride", ctypes.c_uint64),
+                ("n_pages", ctypes.c_uint32), ("page_tokens", ctypes.c_uint32), ("kv_heads", ctypes.c_uint32),
+                ("head_dim", ctypes.c_uint32)]
+
+
+class _CRows(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("row_stride", ctypes.c_uint64), ("head_stride", ctypes.c_uint64)]
+
+
+TYPE_BF16, TYPE_F16, TYPE_F32 = 0, 1, 2
+_TYPES = {torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16, torch.float32: TYPE_F32}
+ATTEND_CAUSAL = 1
+PAGES_MAX_REQUESTS = 4000
+PAGES_REPORT_BYTES = 16
+
+
+class Pages:
+    """A pool of 8-bit cache pages: codes of keys and values (n_pages, kv_heads, page_tokens, head_dim) as
+    uint8 or float8_e4m3fn tensors (any strides whose last is 1), and their scales (n_pages, kv_heads), float32.
+    Holds the tensors; their memory must not be given another use while the pool is in use."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        for t, what in ((k, "k"), (v, "v")):
+            if not t.is_cuda:
+                raise WmError(f"{what} must be a CUDA tensor (there is no CPU path)")
+            if t.dim() != 4 or t.element_size() != 1 or t.stride(3) != 1:
+                raise WmError(f"{what} must be 8-bit codes (n_pages, kv_heads, page_tokens, head_dim) whose channels are contiguous")
+        if k.shape != v.shape or k.stride() != v.stride() or k.device != v.device:
+            raise WmError("keys and values must have the same shape, strides and device")
+        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t.shape != k.shape[:2] or t.dtype != torch.float32 or t.device != k.device or not t.is_contiguous():
+                raise WmError(f"{what} must be a contiguous float32 tensor (n_pages, kv_heads) on the codes' device")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.kv_heads, self.page_tokens, self.head_dim = k.shape
+        self._c = _CPages(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
+                          self.n_pages, self.page_tokens, self.kv_heads, self.head_dim)
+        self._ref = ctypes.addressof(self._c)
+
+
+def new_pages(n_pages: int, page_tokens: int, kv_heads: int, head_dim: int, device="cuda") -> Pages:
+    """A pool with all codes and scales zero."""
+    shape = (n_pages, kv_heads, page_tokens, head_dim)
+    k, v = (torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2))
+    return Pages(k, v, *(torch.zeros(shape[:2], dtype=torch.float32, device=device) for _ in range(2)))
+
+
+def pages_workspace_bytes(head_dim: int) -> int:
+    return int(lib().wm_pages_workspace_bytes(head_dim))
+
+
+def new_pages_workspace(head_dim: int, device="cuda") -> torch.Tensor:
+    """Scratch of wm_pages_attend: calls that share it must be ordered."""
+    n = pages_workspace_bytes(head_dim)
+    if n == 0:
+        raise WmError("bad geometry")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def new_pages_report(device="cuda") -> torch.Tensor:
+    return torch.zeros(PAGES_REPORT_BYTES, dtype=torch.uint8, device=device)
+
+
+def read_pages_report(report: torch.Tensor):
+    """(status name, lowest index concerned or None) of a report; synchronises the current stream."""
+    status, first = report[:8].cpu().view(torch.int32).tolist()
+    return STATUS.get(status, str(status)), (first & 0xFFFFFFFF) - 1 if first else None
+
+
+def _i32(t: torch.Tensor, n, what: str) -> int:
+    if not t.is_cuda:
+        raise WmError(f"{what} must be a CUDA tensor (there is no CPU path)")
+    if t.dtype != torch.int32 or not t.is_contiguous() or (n is not None and t.numel() != n):
+        raise WmError(f"{what} must be a contiguous int32 tensor" + (f" of {n} entries" if n is not None else ""))
+    return t.data_ptr()
+
+
+def _table(t: torch.Tensor, n_requests: int):
+    if not t.is_cuda or t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != n_requests or (t.numel() and t.stride(1) != 1) or \
+            t.stride(0) < t.shape[1]:
+        raise WmError(f"the table must be an int32 CUDA tensor of {n_requests} rows whose entries are contiguous")
+    if t.shape[0] > 1 and t.stride(0) != t.shape[1]:
+        raise WmError("the table must be contiguous")
+    return t.data_ptr(), t.shape[1]
+
+
+def _rows(t: torch.Tensor, heads: int, dim: int, what: str) -> _CRows:
+    if not t.is_cuda:
+        raise WmError(f"{what} must be a CUDA tensor (there is no CPU path)")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.stride(2) != 1 or t.dtype not in _TYPES:
+        raise WmError(f"{what} must be (rows, {heads}, {dim}) in bfloat16, float16 or float32 with contiguous channels")
+    return _CRows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def wm_pages_plan(old_len: torch.Tensor, new_len: torch.Tensor, page_tokens: int, table: torch.Tensor, free_pages: torch.Tensor,
+                  free_count: torch.Tensor, free_count_out: torch.Tensor, start: torch.Tensor, slots: torch.Tensor, report=None,
+                  stream=None) -> None:
+    """Block tables, free list, row offsets and slot map of a step (see include/wm.h).  All tensors are int32;
+    `free_count_out` may be `free_count`."""
+    n = old_len.numel()
+    tab, width = _table(table, n)
+    _check(lib().wm_pages_plan(_i32(old_len, None, "old_len"), _i32(new_len, n, "new_len"), n, page_tokens, free_pages.numel(),
+                               tab, width, _i32(free_pages, None, "free_pages"), _i32(free_count, 1, "free_count"),
+                               _i32(free_count_out, 1, "free_count_out"), _i32(start, n + 1, "start"), _i32(slots, None, "slots"),
+                               slots.numel(), None if report is None else report.data_ptr(), _stream(stream)), "wm_pages_plan")
+
+
+def wm_pages_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, report=None, stream=None) -> None:
+    """Rows of keys and values (rows, kv_heads, head_dim) into the slots of the pool (see include/wm.h)."""
+    ck, cv = (_rows(t, pages.kv_heads, pages.head_dim, what) for t, what in ((k, "k"), (v, "v")))
+    if k.dtype != v.dtype or k.shape[0] != v.shape[0]:
+        raise WmError("k and v must have the same type and number of rows")
+    _check(lib().wm_pages_append(pages._ref, ctypes.byref(ck), ctypes.byref(cv), _TYPES[k.dtype], _i32(slots, k.shape[0], "slots"),
+                                 k.shape[0], None if report is None else report.data_ptr(), _stream(stream)), "wm_pages_append")
+
+
+def wm_pages_attend(pages: Pages, table: torch.Tensor, kv_len: torch.Tensor, q_start: torch.Tensor, q: torch.Tensor,
+                    out: torch.Tensor, workspace: torch.Tensor, lse=None, scale=None, causal: bool = True, window: int = 0,
+                    max_q=None, report=None, stream=None) -> None:
+    """Attention of the rows q (rows, q_heads, head_dim) over the pool into `out` (see include/wm.h).  `scale` is
+    head_dim ** -0.5 unless given; `max_q` the most rows a request has (all of q's unless given)."""
+    n, rows, heads = kv_len.numel(), q.shape[0], q.shape[1] if q.dim() == 3 else 0
+    cq, co = (_rows(t, heads, pages.head_dim, what) for t, what in ((q, "q"), (out, "out")))
+    if out.dtype != q.dtype or out.shape != q.shape:
+        raise WmError("out must have q's type and shape")
+    if lse is not None and (not lse.is_cuda or lse.dtype != torch.float32 or lse.shape != (rows, heads) or not lse.is_contiguous()):
+        raise WmError(f"lse must be a contiguous float32 CUDA tensor ({rows}, {heads})")
+    tab, width = _table(table, n)
+    _check(lib().wm_pages_attend(pages._ref, tab, width, _i32(kv_len, None, "kv_len"), _i32(q_start, n + 1, "q_start"), n,
+                                 ctypes.byref(cq), ctypes.byref(co), _TYPES[q.dtype], None if lse is None else lse.data_ptr(), rows,
+                                 heads, rows if max_q is None else int(max_q),
+                                 pages.head_dim ** -0.5 if scale is None else float(scale), ATTEND_CAUSAL if causal else 0,
+                                 int(window), workspace.data_ptr(), workspace.numel(),
+                                 None if report is None else report.data_ptr(), _stream(stream)), "wm_pages_attend")

@@ -6,7 +6,7 @@ import subprocess
 import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = [os.path.join(HERE, "csrc", "wm_kernels.cu")]
+SRC = [os.path.join(HERE, "csrc", f) for f in ("wm_kernels.cu", "wm_pages.cu")]
 DEPS = [os.path.join(HERE, "csrc", f) for f in sorted(os.listdir(os.path.join(HERE, "csrc")))] + [
     os.path.join(os.path.dirname(HERE), "include", "wm.h")]
 OUT = os.path.join(HERE, "libwm.so")
@@ -24,11 +24,19 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return OUT
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-diag-suppress", "177", "-shared", "-Xcompiler", "-fPIC", "-o", OUT + ".tmp"] + SRC
+           "-diag-suppress", "177", "-Xcompiler", "-fPIC"]
     if verbose:
         cmd.insert(1, "-Xptxas")
         cmd.insert(2, "-v")
-    subprocess.check_call(cmd)
+    # one object per translation unit, compiled side by side
+    objects, running = [], []
+    for src in SRC:
+        obj = OUT[:-3] + "." + os.path.basename(src)[:-3] + ".o"
+        objects.append(obj)
+        running.append(subprocess.Popen(cmd + ["-c", "-o", obj, src]))
+    if any([p.wait() for p in running]):
+        raise subprocess.CalledProcessError(1, cmd)
+    subprocess.check_call([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", OUT + ".tmp"] + objects)
     os.replace(OUT + ".tmp", OUT)
     return OUT
 

@@ -23,6 +23,8 @@
 
 #include "../../include/wm.h"
 #include "wm_device.cuh"
+#include "wm_host.h"
+#include "wm_launch.h"
 
 // The kernels, one file per call (a single translation unit: the host side below launches them).
 #include "wm_layout.cuh"
@@ -75,7 +77,9 @@ struct MainKernelTimer {        // records events around a main kernel when timi
 };
 static DeviceState g_dev[64];
 static std::mutex g_mutex;
-static thread_local uint32_t g_launches = 0;
+thread_local uint32_t g_launches = 0;
+uint32_t wait_budget_ns() { return g_wait_ns.load(std::memory_order_relaxed); }
+uint32_t inject_bits() { return g_inject.load(std::memory_order_relaxed); }
 
 static const DeviceState* device_state()
 {
@@ -125,31 +129,6 @@ static const DeviceState* device_state()
             if (cudaEventCreate(&s.ev[k][j]) != cudaSuccess) return nullptr;
     s.ready = true;
     return &s;
-}
-
-// Launch a kernel that may start before the kernel enqueued just before it on the stream has
-// finished (it waits inside, see grid_dep_wait).
-template <typename... Params, typename... Args>
-static void launch_after(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args&&... args)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
-}
-
-static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-static wm_status launch_status()
-{
-    return cudaGetLastError() == cudaSuccess ? WM_OK : WM_ERR_CUDA;
 }
 
 }  // namespace wm

@@ -1,0 +1,127 @@
+// The paged 8-bit cache: kernels (sm_100a) and C ABI.
+//   wm_pages_plan    : k_pages_plan
+//   wm_pages_append  : k_pages_append
+//   wm_pages_attend  : k_attend_rows
+#include <cstdint>
+#include <cmath>
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include "../../include/wm.h"
+#include "wm_device.cuh"
+#include "wm_host.h"
+#include "wm_launch.h"
+#include "wm_pages.cuh"
+#include "wm_attend.cuh"
+
+namespace wm {
+
+// The pool's geometry: what every call checks before anything is launched.
+static bool pages_ok(const wm_pages* p, uint32_t& shift)
+{
+    if (!p || !p->k || !p->v || !p->k_scale || !p->v_scale) return false;
+    if (!aligned16(p->k) || !aligned16(p->v)) return false;
+    if (((p->page_stride | p->head_stride | p->token_stride) & 15u) != 0) return false;
+    shift = p->page_tokens == 16 ? 4 : p->page_tokens == 32 ? 5 : p->page_tokens == 64 ? 6 : p->page_tokens == 128 ? 7 : 0;
+    if (!shift || (p->head_dim != 64 && p->head_dim != 128)) return false;
+    if (p->token_stride < p->head_dim || p->kv_heads == 0 || p->kv_heads > 1024) return false;
+    if (p->n_pages == 0 || (uint64_t)p->n_pages * p->page_tokens >= (1ull << 31)) return false;
+    return true;
+}
+
+// Rows whose bytes every 16-byte access may touch; `size`: bytes of an element.
+static bool rows_ok(const wm_rows* r, uint32_t size)
+{
+    return r && r->ptr && aligned16(r->ptr) && (r->row_stride * size) % 16 == 0 && (r->head_stride * size) % 16 == 0;
+}
+
+template <typename T>
+static void append_launch(const AppendArgs& a, cudaStream_t s)
+{
+    const dim3 grid(a.n_rows, (2u * a.p.kv_heads + 7u) / 8u);
+    if (a.p.head_dim == 64) launch_after(k_pages_append<T, 64>, grid, 256, 0, s, a);
+    else launch_after(k_pages_append<T, 128>, grid, 256, 0, s, a);
+}
+
+template <typename T>
+static void attend_launch(const AttendArgs& a, cudaStream_t s)
+{
+    const dim3 grid(a.n_rows, a.q_heads);
+    if (a.p.head_dim == 64) launch_after(k_attend_rows<T, 64>, grid, 128, 0, s, a);
+    else launch_after(k_attend_rows<T, 128>, grid, 128, 0, s, a);
+}
+
+}  // namespace wm
+
+using namespace wm;
+
+extern "C" {
+
+wm_status wm_pages_plan(const int32_t* old_len, const int32_t* new_len, uint32_t n_requests, uint32_t page_tokens, uint32_t n_pages,
+                        int32_t* table, uint32_t table_stride, int32_t* free_pages, const uint32_t* free_count,
+                        uint32_t* free_count_out, int32_t* start, int32_t* slots, uint32_t n_slots,
+                        wm_pages_report* report, void* stream)
+{
+    const uint32_t shift = page_tokens == 16 ? 4 : page_tokens == 32 ? 5 : page_tokens == 64 ? 6 : page_tokens == 128 ? 7 : 0;
+    if (!old_len || !new_len || !table || !free_pages || !free_count || !free_count_out || !start || (!slots && n_slots)) return WM_ERR_ARG;
+    if (!shift || n_requests == 0 || n_requests > kMaxRequests || table_stride == 0 || n_slots >= (1u << 31)) return WM_ERR_ARG;
+    if (n_pages == 0 || ((uint64_t)n_pages << shift) >= (1ull << 31) || (uint64_t)n_requests * table_stride >= (1ull << 31)) return WM_ERR_ARG;
+    const PlanArgs a = {old_len, new_len, n_requests, page_tokens, shift, n_pages, table, table_stride, free_pages, free_count,
+                        free_count_out, start, slots, n_slots, report};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const bool small = n_requests <= 1024u && n_slots <= 4096u;
+    launch_after_clustered(small ? k_pages_plan<false> : k_pages_plan<true>, small ? 1 : kPlanBlocks, kPlanThreads,
+                           3u * (n_requests + 1u) * 4u, small ? 1 : kPlanBlocks, s, a);
+    g_launches = 1;
+    return launch_status();
+}
+
+wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows* v, int type, const int32_t* slots, uint32_t n_rows,
+                          wm_pages_report* report, void* stream)
+{
+    uint32_t shift = 0;
+    if (type < WM_TYPE_BF16 || type > WM_TYPE_F32) return WM_ERR_ARG;
+    const uint32_t size = type == WM_TYPE_F32 ? 4 : 2;
+    if (!pages_ok(pages, shift) || !rows_ok(k, size) || !rows_ok(v, size) || !slots || n_rows >= (1u << 31)) return WM_ERR_ARG;
+    g_launches = 0;
+    if (n_rows == 0) return WM_OK;
+    const AppendArgs a = {*pages, shift, {k->ptr, v->ptr}, {k->row_stride, v->row_stride}, {k->head_stride, v->head_stride}, slots, n_rows, report};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (type == WM_TYPE_BF16) append_launch<__nv_bfloat16>(a, s);
+    else if (type == WM_TYPE_F16) append_launch<__half>(a, s);
+    else append_launch<float>(a, s);
+    g_launches = 1;
+    return launch_status();
+}
+
+uint64_t wm_pages_workspace_bytes(uint32_t head_dim)
+{
+    return head_dim == 64 || head_dim == 128 ? 1024 : 0;
+}
+
+wm_status wm_pages_attend(const wm_pages* pages, const int32_t* table, uint32_t table_stride, const int32_t* kv_len,
+                          const int32_t* q_start, uint32_t n_requests, const wm_rows* q, const wm_rows* out, int type, float* lse,
+                          uint32_t n_rows, uint32_t q_heads, uint32_t max_q, float scale, uint32_t options, uint32_t window,
+                          void* workspace, uint64_t workspace_bytes, wm_pages_report* report, void* stream)
+{
+    uint32_t shift = 0;
+    if (!pages_ok(pages, shift) || !rows_ok(q, 2) || !rows_ok(out, 2) || !table || !kv_len || !q_start) return WM_ERR_ARG;
+    if ((type != WM_TYPE_BF16 && type != WM_TYPE_F16) || (options & ~WM_ATTEND_CAUSAL) || (window && !(options & WM_ATTEND_CAUSAL))) return WM_ERR_ARG;
+    if (n_requests == 0 || n_requests > kMaxRequests || table_stride == 0 || (uint64_t)n_requests * table_stride >= (1ull << 31)) return WM_ERR_ARG;
+    if ((uint64_t)table_stride << shift >= (1ull << 31) || n_rows >= (1u << 24) || max_q == 0 || !std::isfinite(scale)) return WM_ERR_ARG;
+    if (q_heads == 0 || q_heads % pages->kv_heads || q_heads / pages->kv_heads > 64u) return WM_ERR_ARG;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < wm_pages_workspace_bytes(pages->head_dim)) return WM_ERR_ARG;
+    g_launches = 0;
+    if (n_rows == 0) return WM_OK;
+    const AttendArgs a = {*pages, shift, table, table_stride, kv_len, q_start, n_requests, q->ptr, out->ptr, q->row_stride, q->head_stride,
+                          out->row_stride, out->head_stride, lse, n_rows, q_heads, q_heads / pages->kv_heads, scale,
+                          options & WM_ATTEND_CAUSAL, window, report};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (type == WM_TYPE_BF16) attend_launch<__nv_bfloat16>(a, s);
+    else attend_launch<__half>(a, s);
+    g_launches = 1;
+    return launch_status();
+}
+
+}  // extern "C"
