@@ -18,6 +18,8 @@ struct AttendArgs {
     uint32_t n_rows, q_heads, group;
     float scale;
     uint32_t causal, window;
+    unsigned char* ws;
+    uint32_t wait_ns, inject;
     wm_pages_report* rep;
 };
 
@@ -25,87 +27,576 @@ __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162f
 __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 __device__ __forceinline__ void from_float(__nv_bfloat16& o, float v) { o = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void from_float(__half& o, float v) { o = __float2half_rn(v); }
-__device__ __forceinline__ float code_value(unsigned char c)
+
+// A request as the kernels see it: `rows` is 0 where there is nothing to do (or the request cannot be answered).
+struct Request {
+    int32_t start, rows, kv;
+    bool ok;
+};
+__device__ __forceinline__ Request request_of(const AttendArgs& a, uint32_t i)
 {
-    const uint32_t h = from_e4m3x2(c);
-    return __half2float(*reinterpret_cast<const __half*>(&h));
+    Request r;
+    r.start = a.q_start[i];
+    const int32_t end = a.q_start[i + 1];
+    r.kv = a.kv_len[i];
+    r.ok = r.start >= 0 && end >= r.start && (uint32_t)end <= a.n_rows && r.kv >= 0 && (uint32_t)r.kv <= (a.table_stride << a.page_shift);
+    r.rows = r.ok ? end - r.start : 0;
+    return r;
 }
 
-// A block per (row, query head): the scores of 128 tokens, then their values.
-template <typename T, int D>
-__global__ void __launch_bounds__(128)
-k_attend_rows(AttendArgs a)
+// ------------------------------------------------------------------ few rows: the cache is read once, split over all SMs
+//
+// For one key head the rows of a request (its queries times the heads that share the key head) are few, and every byte of
+// the cache is used for few products: reading it is what the time goes to.  So codes go from memory into the tensor cores as they
+// are, without passing a register: the tile of 128 tokens is the MMA's 128-row operand, and the few queries its columns.
+//   scores   S[token][column] = K[token][:] . Q[column][:]           (K as it lies: K-major)
+//   outputs  O[channel][column] = sum_token V[token][channel] P[token][column]   (V as it lies: MN-major)
+// Both are e4m3 x e4m3 with f32 sums.  Queries and weights have more than e4m3's four bits, so each is held as a sum of pieces
+// in columns of their own, every piece the rounded remainder of the one before times 16: 4 bits a piece, two for a bf16 query
+// (8 bits: exact for elements above 2^-18 of the row's largest), three for f16's 11 bits and for the weights.  The columns are
+// there anyway: an MMA of 128 rows costs as much for 16 columns as for 8.
+// A page's scales are applied in f32: the key's to the score, the value's to the weight (as an addition of its logarithm in the
+// exponent, so that weights keep their bits however far apart the scales are): p' = 2^(x + log2 vs - R) <= 1 with a running
+// maximum R of its own beside the softmax's m, and out = O 2^(R - m) / l.
+//
+// Work is dealt out in tiles: all units (request, key head, tile of rows) one behind the other give T tiles of 128 tokens, worker
+// w (a block; two on an SM) takes tiles w T / W .. (w + 1) T / W.  A unit that ends inside a worker's share is finished there; one that is cut
+// leaves (o, m, R, l) in the workspace, and k_attend_join puts the pieces together in the workers' order (no atomics: the
+// result does not depend on timing).
+
+template <typename T, int D, int RT> struct Few {
+    static constexpr uint32_t kQP = sizeof(T) == 2 && std::is_same<T, __half>::value ? 3 : 2;     // pieces of a query
+    static constexpr uint32_t kNQ = (RT * kQP + 15) / 16 * 16, kNP = (RT * 3 + 15) / 16 * 16;     // columns of S and of O
+    static constexpr uint32_t kWP = kNP <= 32 ? 32 : kNP <= 64 ? 64 : 128;                       // bytes of a token's row of P
+    static constexpr uint32_t kSwP = kWP == 32 ? kSw32 : kWP == 64 ? kSw64 : kSw128, kSwD = D == 128 ? kSw128 : kSw64;
+    static constexpr uint32_t kHalf = 128 * D, kStage = 2 * kHalf;                                 // a tile's keys; with its values
+    // three tiles of keys and values in flight, two where three would not leave room for a second block on the SM
+    static constexpr uint32_t kRest = kNQ * D + 128 * kWP + 140 * RT + 2048;
+    static constexpr uint32_t kStages = (3 * 32768 + kRest <= 115712 ? 3 : 2) * (128 / D);
+    static constexpr uint32_t kCols = kNQ + kNP <= 64 ? 64 : kNQ + kNP <= 128 ? 128 : 256;
+    // shared memory, from a 1024-byte boundary on
+    static constexpr uint32_t oQ = kStages * kStage, oP = oQ + (kNQ * D + 1023) / 1024 * 1024, oMisc = oP + 128 * kWP;
+    struct Misc {
+        unsigned long long kfull[kStages], vfull[kStages], empty[kStages], sbar, obar, fin;
+        float2 scales[kStages][8];        // (key scale, value scale) of the tile's pages
+        float top[4][RT][2];              // a warp's largest score and largest weighted score
+        alignas(16) float state[4][RT][4];            // per warp: m, R, factors of l and of o
+        float f[RT];                      // scale log2(e) / the query row's factor
+        float sum[4][RT];
+        unsigned long long scan[4], total;
+        unsigned long long first_prefix;
+        uint32_t first_req, tmem, dead, poison;
+    };
+    static constexpr uint32_t kSmem = oMisc + (uint32_t)sizeof(Misc) + 1024;
+};
+
+constexpr uint32_t kMaxWorkers = 512, kPartRows = 32;
+// A cut unit's description, left by the worker that has its first tile.
+struct Cut {
+    uint32_t valid, req, head, rt, last, slot, pad[2];
+};
+constexpr uint32_t kPartFloats = kPartRows * 128 + kPartRows * 4;
+__host__ __device__ constexpr uint64_t attend_workspace() { return kMaxWorkers * sizeof(Cut) + (uint64_t)kMaxWorkers * 2 * kPartFloats * 4; }
+__device__ __forceinline__ float* part_of(unsigned char* ws, uint32_t worker, uint32_t slot)
 {
-    __shared__ float s_q[D], s_p[128], s_vs[128], s_red[8];
-    __shared__ int64_t s_at[128];
-    __shared__ uint32_t s_req, s_bad;
-    const uint32_t tid = threadIdx.x, row = blockIdx.x, qh = blockIdx.y, h = qh / a.group;
+    return reinterpret_cast<float*>(ws + kMaxWorkers * sizeof(Cut)) + (size_t)(worker * 2 + slot) * kPartFloats;
+}
+
+struct UnitShape {
+    uint32_t row_tiles, j0, nt;
+    unsigned long long tiles;
+};
+template <int RT> __device__ __forceinline__ UnitShape shape_of(const AttendArgs& a, const Request& r)
+{
+    UnitShape u;
+    u.row_tiles = ((uint32_t)r.rows * a.group + RT - 1u) / RT;
+    const int32_t lo = a.window ? max(0, r.kv - r.rows + 1 - (int32_t)min(a.window, 0x7FFFFFFFu)) : 0;
+    u.j0 = (uint32_t)lo / 128u;
+    const uint32_t end = ((uint32_t)r.kv + 127u) / 128u;
+    u.nt = end > u.j0 ? end - u.j0 : 1u;
+    u.tiles = (unsigned long long)a.p.kv_heads * u.row_tiles * u.nt;
+    return u;
+}
+
+template <typename T> __device__ __forceinline__ void store_out(const AttendArgs& a, uint32_t row, uint32_t qh, uint32_t d, float v)
+{
+    T r;
+    from_float(r, v);
+    static_cast<T*>(a.out)[row * a.o_row + qh * a.o_head + d] = r;
+}
+
+template <typename T, int D, int RT>
+__global__ void __launch_bounds__(160, 2)
+k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap)
+{
+    using F = Few<T, D, RT>;
+    extern __shared__ unsigned char few_smem[];
+    unsigned char* base = few_smem + ((1024u - ((uint32_t)__cvta_generic_to_shared(few_smem) & 1023u)) & 1023u);
+    const uint32_t base_s = (uint32_t)__cvta_generic_to_shared(base);
+    typename F::Misc& M = *reinterpret_cast<typename F::Misc*>(base + F::oMisc);
+    const uint32_t tid = threadIdx.x, lane = tid % 32, warp = warp_uniform(tid / 32);
+    auto bar = [&](const unsigned long long& b) { return (uint32_t)__cvta_generic_to_shared(&b); };
+
+    if (tid == 0) {
+        for (uint32_t s = 0; s < F::kStages; s++) { mbar_init(&M.kfull[s], 1); mbar_init(&M.vfull[s], 1); mbar_init(&M.empty[s], 1); }
+        mbar_init(&M.sbar, 1);
+        mbar_init(&M.obar, 1);
+        mbar_init(&M.fin, 1);
+        M.dead = 0;
+        M.poison = 0;
+    }
+    if (warp == 4) tmem_alloc<F::kCols>((uint32_t)__cvta_generic_to_shared(&M.tmem));
     grid_dep_wait();
     grid_dep_launch();
-    if (tid == 0) { s_req = 0xFFFFFFFFu; s_bad = 0; }
+
+    // this worker's share: each of 128 threads sums the tiles of some consecutive requests
+    const uint32_t per = (a.n + 127u) / 128u;
+    unsigned long long mine = 0, incl = 0;
+    if (warp < 4) {
+        for (uint32_t i = tid * per; i < min((tid + 1) * per, a.n); i++) {
+            const Request r = request_of(a, i);
+            if (!r.ok && blockIdx.x == 0) pages_fault(a.rep, WM_ERR_ARG, i);
+            if (r.rows) mine += shape_of<RT>(a, r).tiles;
+        }
+        incl = mine;
+#pragma unroll
+        for (uint32_t d = 1; d < 32; d <<= 1) {
+            const unsigned long long o = __shfl_up_sync(0xFFFFFFFFu, incl, d);
+            if (lane >= d) incl += o;
+        }
+        if (lane == 31) M.scan[warp] = incl;
+    }
+    tmem_fence_before_sync();
     __syncthreads();
-    for (uint32_t i = tid; i < a.n; i += 128) {
-        const int32_t s = a.q_start[i], e = a.q_start[i + 1], kv = a.kv_len[i];
-        const bool ok = s >= 0 && e >= s && (uint32_t)e <= a.n_rows && kv >= 0 && (uint32_t)kv <= (a.table_stride << a.page_shift);
-        if (!ok) { if (row == 0 && qh == 0) pages_fault(a.rep, WM_ERR_ARG, i); }
-        else if ((int32_t)row >= s && (int32_t)row < e) s_req = i;
+    tmem_fence_after_sync();
+    const uint32_t tmem = M.tmem, tS = tmem, tO = tmem + F::kNQ;
+    const unsigned long long total = M.scan[0] + M.scan[1] + M.scan[2] + M.scan[3];
+    const unsigned long long workers = min((unsigned long long)gridDim.x, total);       // so that every share has a tile
+    const unsigned long long t_begin = blockIdx.x < workers ? blockIdx.x * total / workers : total;
+    const unsigned long long t_end = blockIdx.x < workers ? (blockIdx.x + 1ull) * total / workers : total;
+    if (warp < 4) {
+        for (uint32_t w = 0; w < warp; w++) incl += M.scan[w];
+        unsigned long long at = incl - mine;
+        if (at <= t_begin && t_begin < incl) {
+            uint32_t i = tid * per;
+            for (;; i++) {
+                const Request r = request_of(a, i);
+                const unsigned long long t = r.rows ? shape_of<RT>(a, r).tiles : 0;
+                if (t_begin < at + t) break;
+                at += t;
+            }
+            M.first_req = i;
+            M.first_prefix = at;
+        }
+    }
+    if (tid == 0) {
+        Cut none = {};
+        reinterpret_cast<Cut*>(a.ws)[blockIdx.x] = none;
     }
     __syncthreads();
-    if (s_req == 0xFFFFFFFFu) return;
-    const uint32_t i = s_req;
-    const int64_t kv = a.kv_len[i], pos = kv - (a.q_start[i + 1] - (int32_t)row);
-    int64_t lo = 0, hi = kv;
-    if (a.causal) hi = pos + 1 < hi ? pos + 1 : hi;
-    if (a.window) lo = pos + 1 - (int64_t)a.window > 0 ? pos + 1 - (int64_t)a.window : 0;
-    for (uint32_t d = tid; d < D; d += 128) s_q[d] = to_float(static_cast<const T*>(a.q)[row * a.q_row + qh * a.q_head + d]) * a.scale;
-    float m = -INFINITY, l = 0.0f, o = 0.0f;
-    for (int64_t t0 = lo; t0 < hi; t0 += 128) {
-        __syncthreads();
-        const int64_t t = t0 + tid;
-        float s = -INFINITY, vs = 0.0f;
-        int64_t at = -1;
-        if (t < hi) {
-            const int32_t page = a.table[(size_t)i * a.table_stride + (t >> a.page_shift)];
-            if ((uint32_t)page >= a.p.n_pages) {
-                s = vs = NAN;
-                pages_fault(a.rep, WM_ERR_ARG, i);
-            } else {
-                at = (int64_t)page * a.p.page_stride + h * a.p.head_stride + (t & (a.p.page_tokens - 1u)) * a.p.token_stride;
-                const unsigned char* k = static_cast<const unsigned char*>(a.p.k) + at;
-                float sum = 0.0f;
-                for (int d = 0; d < D; d++) sum += s_q[d] * code_value(k[d]);
-                s = sum * a.p.k_scale[(size_t)page * a.p.kv_heads + h];
-                vs = a.p.v_scale[(size_t)page * a.p.kv_heads + h];
+
+    if (t_begin < t_end) {
+        uint32_t req = M.first_req;
+        unsigned long long prefix = M.first_prefix, t = t_begin;
+        if (warp == 4) {
+            // ---- the copies: a lane per page of the tile
+            const uint32_t pages = 128u >> a.page_shift;
+            uint32_t stage = 0, phase = 0;
+            while (t < t_end) {
+                const Request r = request_of(a, req);
+                const UnitShape u = r.rows ? shape_of<RT>(a, r) : UnitShape{0, 0, 1, 0};
+                if (t >= prefix + u.tiles) { prefix += u.tiles; req++; continue; }
+                const unsigned long long off = t - prefix;
+                const uint32_t unit = (uint32_t)(off / u.nt), j = (uint32_t)(off % u.nt), head = unit / u.row_tiles;
+                const uint32_t count = (uint32_t)min((unsigned long long)(u.nt - j), t_end - t);
+                const int32_t* row = a.table + (size_t)req * a.table_stride;
+                for (uint32_t c = 0; c < count; c++) {
+                    const uint32_t first = (u.j0 + j + c) * 128u;
+                    const uint32_t tokens = first < (uint32_t)r.kv ? min(128u, (uint32_t)r.kv - first) : 0u;
+                    const uint32_t n = (tokens + a.p.page_tokens - 1u) >> a.page_shift;       // pages with tokens
+                    int32_t page = 0;
+                    float2 sc = make_float2(0.0f, 0.0f);
+                    if (lane < n) {
+                        page = row[(first >> a.page_shift) + lane];
+                        if ((uint32_t)page < a.p.n_pages) {
+                            const size_t at = (size_t)page * a.p.kv_heads + head;
+                            sc = make_float2(a.p.k_scale[at], a.p.v_scale[at]);
+                        } else {
+                            sc = make_float2(NAN, 0.0f);       // NaN where a row sees it; what it loads does not matter
+                            page = 0;
+                            pages_fault(a.rep, WM_ERR_ARG, req);
+                        }
+                    }
+                    mbar_wait(bar(M.empty[stage]), phase ^ 1u, a.wait_ns, &M.dead);
+                    if (lane < pages) M.scales[stage][lane] = sc;
+                    __syncwarp();
+                    const uint32_t bytes = (n << a.page_shift) * D;
+                    const bool copy = !(a.inject & kInjectNoCopy);
+                    if (lane == 0) {
+                        if (copy || n == 0) { mbar_expect(bar(M.kfull[stage]), bytes); mbar_expect(bar(M.vfull[stage]), bytes); }
+                    }
+                    __syncwarp();
+                    if (lane < n && copy) {
+                        const uint32_t dst = base_s + stage * F::kStage + (lane << a.page_shift) * D;
+                        tile_load4(dst, &kmap, 0, (int32_t)head, page, bar(M.kfull[stage]));
+                        tile_load4(dst + F::kHalf, &vmap, 0, (int32_t)head, page, bar(M.vfull[stage]));
+                    }
+                    if (++stage == F::kStages) { stage = 0; phase ^= 1u; }
+                }
+                t += count;
+            }
+            // nothing may still be on its way into this block's shared memory when it leaves
+            if (*(volatile uint32_t*)&M.dead && !(a.inject & kInjectNoCopy)) {
+                for (uint32_t s = 0; s < F::kStages; s++) {
+                    const uint32_t t0 = now_ns();
+                    const uint32_t parity = s < stage ? phase : phase ^ 1u;
+                    while (!(mbar_try(bar(M.kfull[s]), parity) && mbar_try(bar(M.vfull[s]), parity)) && now_ns() - t0 < a.wait_ns) {}
+                }
+            }
+        } else {
+            // ---- scores, softmax, outputs: thread = token of the tile, then channel
+            uint32_t stage = 0, kphase = 0, sphase = 0, ophase = 0;
+            const uint32_t lane_t = tmem + ((warp * 32u) << 16);
+            const uint32_t qs = base_s + F::oQ, ps = base_s + F::oP;
+            auto issue_scores = [&](uint32_t st) {
+                const uint32_t k0 = base_s + st * F::kStage;
+#pragma unroll
+                for (uint32_t kk = 0; kk < D / 32; kk++)
+                    mma_f8(tS, smem_desc(k0 + kk * 32u, 16, 8 * D, F::kSwD), smem_desc(qs + kk * 32u, 16, 8 * D, F::kSwD),
+                           mma_desc(128, F::kNQ, false, false), kk > 0);
+                mma_commit(bar(M.sbar));
+            };
+            while (t < t_end) {
+                const Request r = request_of(a, req);
+                const UnitShape u = r.rows ? shape_of<RT>(a, r) : UnitShape{0, 0, 1, 0};
+                if (t >= prefix + u.tiles) { prefix += u.tiles; req++; continue; }
+                const unsigned long long off = t - prefix;
+                const uint32_t unit = (uint32_t)(off / u.nt), j = (uint32_t)(off % u.nt), head = unit / u.row_tiles, rt = unit % u.row_tiles;
+                const uint32_t count = (uint32_t)min((unsigned long long)(u.nt - j), t_end - t);
+                const uint32_t row0 = rt * RT, rows = min((uint32_t)RT, (uint32_t)r.rows * a.group - row0);
+                // what the unit's first and last row see: [lo, hi)
+                const int32_t pos0 = r.kv - r.rows + (int32_t)(row0 / a.group), pos1 = r.kv - r.rows + (int32_t)((row0 + rows - 1u) / a.group);
+                const int32_t win = (int32_t)min(a.window, 0x7FFFFFFFu);
+                auto lo_of = [&](int32_t pos) { return win ? max(0, pos + 1 - win) : 0; };
+                auto hi_of = [&](int32_t pos) { return a.causal ? min(r.kv, max(0, pos + 1)) : r.kv; };
+                const int32_t any_lo = lo_of(pos0), any_hi = hi_of(pos1), all_lo = lo_of(pos1), all_hi = hi_of(pos0);
+
+                // the queries' pieces: TPR threads a row
+                {
+                    constexpr uint32_t TPR = 128 / RT, EPT = D / TPR;
+                    const uint32_t rr = tid / TPR, part = tid % TPR;
+                    float x[EPT];
+                    if (rr < rows) {
+                        const uint32_t gr = row0 + rr, qrow = (uint32_t)r.start + gr / a.group, qh = head * a.group + gr % a.group;
+                        const T* src = static_cast<const T*>(a.q) + (size_t)qrow * a.q_row + (size_t)qh * a.q_head + part * EPT;
+#pragma unroll
+                        for (uint32_t e = 0; e < EPT; e += 4) load_row<T, 4>(src + e, *reinterpret_cast<float (*)[4]>(&x[e]));
+                    } else {
+#pragma unroll
+                        for (uint32_t e = 0; e < EPT; e++) x[e] = 0.0f;
+                    }
+                    uint32_t top = 0;
+#pragma unroll
+                    for (uint32_t e = 0; e < EPT; e++) top = max(top, __float_as_uint(fabsf(x[e])));
+#pragma unroll
+                    for (uint32_t d = 1; d < TPR; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+                    // a power of two that brings the row's largest element to 128 .. 256 (NaN where the row is not finite)
+                    const int e = min(max((int)(top >> 23) - 127, -100), 127);
+                    const float up = top >= 0x7F800000u ? NAN : __uint_as_float((uint32_t)(127 + 7 - e) << 23);
+                    const float down = __uint_as_float((uint32_t)(127 - 7 + e) << 23);
+                    if (part == 0) M.f[rr] = a.scale * 1.4426950408889634f * (top >= 0x7F800000u ? NAN : down);
+#pragma unroll
+                    for (uint32_t p = 0; p < F::kQP; p++) {
+                        const uint32_t n = p * RT + rr;
+#pragma unroll
+                        for (uint32_t e4 = 0; e4 < EPT; e4 += 4) {
+                            uint32_t w = 0;
+#pragma unroll
+                            for (uint32_t k = 0; k < 4; k += 2) {
+                                float& x0 = x[e4 + k];
+                                float& x1 = x[e4 + k + 1];
+                                if (p == 0) { x0 *= up; x1 *= up; }
+                                const uint32_t c = to_e4m3x2(x0, x1), h = from_e4m3x2(c);
+                                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                                x0 = (x0 - back.x) * 16.0f;
+                                x1 = (x1 - back.y) * 16.0f;
+                                w |= c << (8 * k);
+                            }
+                            const uint32_t byte = n * D + part * EPT + e4;
+                            sts_now(qs + (byte ^ (((byte >> 7) & (D == 128 ? 7u : 3u)) << 4)), w);
+                        }
+                    }
+                }
+                async_proxy_fence();
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+                if (tid == 0) {
+                    tmem_fence_after_sync();
+                    mbar_wait(bar(M.kfull[stage]), kphase, a.wait_ns, &M.dead);
+                    issue_scores(stage);
+                }
+
+                float o[RT], l[RT];
+#pragma unroll
+                for (uint32_t i = 0; i < RT; i++) { o[i] = 0.0f; l[i] = 0.0f; }
+                float m_run = -INFINITY, r_run = -INFINITY;       // of row `lane`, the same in every warp
+                for (uint32_t c = 0; c < count; c++) {
+                    const int32_t t0 = (int32_t)((u.j0 + j + c) * 128u), tok = t0 + (int32_t)tid;
+                    mbar_wait(bar(M.sbar), sphase, a.wait_ns, &M.dead);
+                    sphase ^= 1u;
+                    tmem_fence_after_sync();
+                    mbar_wait(bar(M.kfull[stage]), kphase, a.wait_ns, &M.dead);   // (long since done: for the scales behind it)
+                    const float2 sc = M.scales[stage][tid >> a.page_shift];
+                    float x[RT];
+                    {
+                        float s[F::kNQ];
+#pragma unroll
+                        for (uint32_t i = 0; i < F::kNQ; i += 8) tmem_read8(lane_t + i, &s[i]);
+                        tmem_wait_loads();
+#pragma unroll
+                        for (uint32_t i = 0; i < RT; i++) {
+                            float v = s[RT + i];
+                            if (F::kQP == 3) v = fmaf(s[2 * RT + i], 0.0625f, v);
+                            x[i] = fmaf(v, 0.0625f, s[i]) * (M.f[i] * sc.x);
+                        }
+                    }
+                    const bool whole = t0 >= all_lo && t0 + 128 <= all_hi;      // every row sees every token
+                    if (!whole) {
+                        uint32_t jq = row0 / a.group, g = row0 % a.group;
+#pragma unroll
+                        for (uint32_t i = 0; i < RT; i++) {
+                            const int32_t pos = r.kv - r.rows + (int32_t)jq;
+                            if (!(tok >= lo_of(pos) && tok < hi_of(pos))) x[i] = -INFINITY;
+                            if (++g == a.group) { g = 0; jq++; }
+                        }
+                    }
+                    const float lv = log2f(sc.y);
+                    {
+                        float mt = -INFINITY, mr = -INFINITY;
+#pragma unroll
+                        for (uint32_t i = 0; i < RT; i++) {
+                            const float v = warp_max(x[i]), w = warp_max(x[i] + lv);
+                            if (lane == i) { mt = v; mr = w; }
+                        }
+                        if (lane < RT) *reinterpret_cast<float2*>(M.top[warp][lane]) = make_float2(mt, mr);
+                    }
+                    asm volatile("bar.sync 1, 128;" ::: "memory");
+                    if (lane < RT) {
+                        float mt = m_run, mr = r_run, mo = -INFINITY;
+#pragma unroll
+                        for (uint32_t w = 0; w < 4; w++) {
+                            const float2 v = *reinterpret_cast<const float2*>(M.top[w][lane]);
+                            mt = fmaxf(mt, v.x);
+                            mo = fmaxf(mo, v.y);
+                        }
+                        mr = fmaxf(mr, mo);
+                        const float mb = mt == -INFINITY ? 0.0f : mt, rb = mr == -INFINITY ? 0.0f : mr, ob = mo == -INFINITY ? 0.0f : mo;
+                        // what exponents refer to, and the factors of l, of o and of this tile's outputs
+                        *reinterpret_cast<float4*>(M.state[warp][lane]) = make_float4(mb, ob - 8.0f, exp2_fast(m_run - mb), exp2_fast(r_run - rb));
+                        M.sum[warp][lane] = exp2_fast(ob - 8.0f - rb);
+                        m_run = mt;
+                        r_run = mr;
+                    }
+                    __syncwarp();
+                    // weights: l in f32, pieces of p' 2^8 into P
+                    uint32_t piece[3][RT / 4];
+#pragma unroll
+                    for (uint32_t i = 0; i < RT; i += 2) {
+                        const float4 s0 = *reinterpret_cast<const float4*>(M.state[warp][i]), s1 = *reinterpret_cast<const float4*>(M.state[warp][i + 1]);
+                        l[i] = fmaf(l[i], s0.z, exp2_fast(x[i] - s0.x));
+                        l[i + 1] = fmaf(l[i + 1], s1.z, exp2_fast(x[i + 1] - s1.x));
+                        float y0 = exp2_fast(x[i] + lv - s0.y), y1 = exp2_fast(x[i + 1] + lv - s1.y);
+                        o[i] *= s0.w;
+                        o[i + 1] *= s1.w;
+#pragma unroll
+                        for (uint32_t p = 0; p < 3; p++) {
+                            const uint32_t cc = to_e4m3x2(y0, y1), h = from_e4m3x2(cc);
+                            const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                            y0 = (y0 - back.x) * 16.0f;
+                            y1 = (y1 - back.y) * 16.0f;
+                            if (i % 4 == 0) piece[p][i / 4] = cc; else piece[p][i / 4] |= cc << 16;
+                        }
+                    }
+                    {
+                        uint32_t w[F::kWP / 4];
+#pragma unroll
+                        for (uint32_t i = 0; i < F::kWP / 4; i++) w[i] = 0;
+#pragma unroll
+                        for (uint32_t p = 0; p < 3; p++)
+#pragma unroll
+                            for (uint32_t i = 0; i < RT / 4; i++) w[p * (RT / 4) + i] = piece[p][i];
+                        const uint32_t swz = F::kWP == 128 ? tid & 7u : F::kWP == 64 ? (tid >> 1) & 3u : (tid >> 2) & 1u;
+#pragma unroll
+                        for (uint32_t ch = 0; ch < F::kNP / 16; ch++)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ps + tid * F::kWP + ((ch ^ swz) << 4)), "r"(w[4 * ch]),
+                                         "r"(w[4 * ch + 1]), "r"(w[4 * ch + 2]), "r"(w[4 * ch + 3]) : "memory");
+                    }
+                    // values that not every row sees must not meet the others' zero weights as NaN: tokens that no row sees are cleared,
+                    // NaN codes of tokens that some rows see are taken out and put into those rows' outputs below
+                    uint32_t nan_at[D / 32];
+                    if (!whole) {
+                        mbar_wait(bar(M.vfull[stage]), kphase, a.wait_ns, &M.dead);
+                        const uint32_t v0 = base_s + stage * F::kStage + F::kHalf + tid * D;
+                        const bool any = tok >= any_lo && tok < any_hi, all = tok >= all_lo && tok < all_hi;
+#pragma unroll
+                        for (uint32_t i = 0; i < D / 32; i++) nan_at[i] = 0;
+                        if (!any) {
+#pragma unroll
+                            for (uint32_t i = 0; i < D; i += 16)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v0 + i), "r"(0u) : "memory");
+                        } else if (!all) {
+                            uint32_t found = 0;
+#pragma unroll
+                            for (uint32_t i = 0; i < D; i += 4) {
+                                // (the word's place among the channels: undo the swizzle)
+                                const uint32_t at = tid * D + i, word = (at ^ (((at >> 7) & (D == 128 ? 7u : 3u)) << 4)) - tid * D;
+                                const uint32_t v = lds_now<0>(v0 + word);
+                                const uint32_t is = __vcmpeq4(v & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                                if (is) {
+                                    found = 1;
+                                    sts_now(v0 + word, v & ~is);
+                                    nan_at[i / 32] |= ((is & 1u) | (is >> 7 & 2u) | (is >> 14 & 4u) | (is >> 21 & 8u)) << (i % 32);
+                                }
+                            }
+                            if (found) M.poison = 1u;
+                        }
+                    }
+                    async_proxy_fence();
+                    tmem_fence_before_sync();
+                    asm volatile("bar.sync 1, 128;" ::: "memory");
+                    const uint32_t next = stage + 1 == F::kStages ? 0 : stage + 1, next_phase = next ? kphase : kphase ^ 1u;
+                    const bool poison = *(volatile uint32_t*)&M.poison;
+                    if (tid == 0) {
+                        tmem_fence_after_sync();
+                        mbar_wait(bar(M.vfull[stage]), kphase, a.wait_ns, &M.dead);
+                        const uint32_t v0 = base_s + stage * F::kStage + F::kHalf;
+#pragma unroll
+                        for (uint32_t kk = 0; kk < 4; kk++)
+                            mma_f8(tO, smem_desc(v0 + kk * 32u * D, 0, 8 * D, F::kSwD), smem_desc(ps + kk * 32u * F::kWP, 0, 8 * F::kWP, F::kSwP),
+                                   mma_desc(128, F::kNP, true, true), kk > 0);
+                        mma_commit(bar(M.obar));
+                        mma_commit(bar(M.empty[stage]));
+                        if (c + 1 < count) {
+                            mbar_wait(bar(M.kfull[next]), next_phase, a.wait_ns, &M.dead);
+                            issue_scores(next);
+                        }
+                    }
+                    mbar_wait(bar(M.obar), ophase, a.wait_ns, &M.dead);
+                    ophase ^= 1u;
+                    tmem_fence_after_sync();
+                    {
+                        float s[F::kNP];
+#pragma unroll
+                        for (uint32_t i = 0; i < F::kNP; i += 8) tmem_read8(lane_t + F::kNQ + i, &s[i]);
+                        tmem_wait_loads();
+#pragma unroll
+                        for (uint32_t i = 0; i < RT; i++)
+                            o[i] = fmaf(fmaf(fmaf(s[2 * RT + i], 0.0625f, s[RT + i]), 0.0625f, s[i]), M.sum[warp][i], o[i]);
+                    }
+                    if (poison) {                          // rare: the marks through P's memory (its MMAs are done)
+#pragma unroll
+                        for (uint32_t i = 0; i < D / 32; i++) sts_now(ps + tid * 16u + 4u * i, whole ? 0u : nan_at[i]);
+                        asm volatile("bar.sync 1, 128;" ::: "memory");
+                        const uint32_t d = tid % D;
+                        for (uint32_t k = 0; k < 128; k++) {
+                            if (!(lds_now<0>(ps + k * 16u + 4u * (d / 32u)) >> (d % 32u) & 1u)) continue;
+                            uint32_t jq = row0 / a.group, g = row0 % a.group;
+#pragma unroll
+                            for (uint32_t i = 0; i < RT; i++) {
+                                const int32_t pos = r.kv - r.rows + (int32_t)jq;
+                                if (t0 + (int32_t)k >= lo_of(pos) && t0 + (int32_t)k < hi_of(pos)) o[i] = NAN;
+                                if (++g == a.group) { g = 0; jq++; }
+                            }
+                        }
+                        if (tid == 0) M.poison = 0;
+                        asm volatile("bar.sync 1, 128;" ::: "memory");
+                    }
+                    stage = next;
+                    kphase = next_phase;
+                }
+
+                // the end of the unit's part: l over the threads, then the outputs or the workspace
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll
+                for (uint32_t i = 0; i < RT; i++) {
+                    float v = l[i];
+#pragma unroll
+                    for (uint32_t d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+                    if (lane == i) M.sum[warp][i] = v;
+                }
+                if (lane < RT) *reinterpret_cast<float2*>(M.state[warp][lane]) = make_float2(m_run, r_run);
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+                const bool dead = *(volatile uint32_t*)&M.dead;
+                const bool full = count == u.nt;
+                const uint32_t slot = t == t_begin ? 0 : 1;
+                float* part = part_of(a.ws, blockIdx.x, slot);
+#pragma unroll
+                for (uint32_t i = 0; i < RT; i++) {
+                    if (i >= rows) break;
+                    const float2 mr = *reinterpret_cast<const float2*>(M.state[warp][i]);
+                    float sum = (M.sum[0][i] + M.sum[1][i]) + (M.sum[2][i] + M.sum[3][i]);
+                    if (dead) sum = NAN;
+                    if (full) {
+                        const uint32_t gr = row0 + i, qrow = (uint32_t)r.start + gr / a.group, qh = head * a.group + gr % a.group;
+                        const float v = sum == 0.0f ? 0.0f : o[i] * exp2_fast(mr.y == -INFINITY ? 0.0f : mr.y - mr.x) / sum;
+                        if (tid < D) store_out<T>(a, qrow, qh, tid, v);
+                        if (tid == 0 && a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = sum == 0.0f ? -INFINITY : (mr.x + log2f(sum)) * 0.6931471805599453f;
+                    } else {
+                        if (tid < D) part[i * D + tid] = o[i];
+                        if (tid == 0) *reinterpret_cast<float4*>(part + kPartRows * 128 + 4 * i) = make_float4(mr.x, mr.y, sum, 0.0f);
+                    }
+                }
+                if (!full && j == 0 && tid == 0) {
+                    // the worker that has the unit's last tile
+                    const unsigned long long last = t + u.nt - 1;
+                    Cut cut = {1u, req, head, rt, (uint32_t)(((last + 1) * workers - 1) / total), slot, {0, 0}};
+                    reinterpret_cast<Cut*>(a.ws)[blockIdx.x] = cut;
+                }
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+                t += count;
             }
         }
-        float top = s;
-        for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-        if (tid % 32 == 0) s_red[tid / 32] = top;
-        __syncthreads();
-        top = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-        const float m1 = fmaxf(m, top), base = m1 == -INFINITY ? 0.0f : m1;
-        const float keep = __expf(m - base), p = t < hi ? __expf(s - base) : 0.0f;
-        float sum = p;
-        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-        if (tid % 32 == 0) s_red[4 + tid / 32] = sum;
-        s_p[tid] = p; s_vs[tid] = vs; s_at[tid] = at;
-        __syncthreads();
-        l = l * keep + ((s_red[4] + s_red[5]) + (s_red[6] + s_red[7]));
+    }
+    if (tid == 0 && *(volatile uint32_t*)&M.dead) {
+        pages_fault(a.rep, WM_ERR_TIMEOUT, 0);
+        mma_commit(bar(M.fin));                            // what was issued is done before the tensor memory is handed back
+        const uint32_t t0 = now_ns();
+        while (!mbar_try(bar(M.fin), 0) && now_ns() - t0 < a.wait_ns) {}
+    }
+    tmem_fence_before_sync();
+    __syncthreads();
+    if (warp == 4) {
+        tmem_fence_after_sync();
+        tmem_free<F::kCols>(tmem);
+    }
+}
+
+// The cut units' parts put together: block (worker, row).
+template <typename T, int D, int RT>
+__global__ void __launch_bounds__(D)
+k_attend_join(AttendArgs a)
+{
+    grid_dep_wait();
+    grid_dep_launch();
+    const uint32_t w0 = blockIdx.x, i = blockIdx.y, d = threadIdx.x;
+    const Cut cut = reinterpret_cast<const Cut*>(a.ws)[w0];
+    if (!cut.valid) return;
+    const Request r = request_of(a, cut.req);
+    const uint32_t gr = cut.rt * RT + i;
+    if (gr >= (uint32_t)r.rows * a.group) return;
+    float m = -INFINITY, R = -INFINITY, l = 0.0f, o = 0.0f;
+    for (uint32_t w = w0; w <= cut.last; w++) {
+        const float* part = part_of(a.ws, w, w == w0 ? cut.slot : 0u);
+        const float4 s = *reinterpret_cast<const float4*>(part + kPartRows * 128 + 4 * i);
+        const float v = part[i * D + d];
+        const float m1 = fmaxf(m, s.x), R1 = fmaxf(R, s.y), mb = m1 == -INFINITY ? 0.0f : m1, rb = R1 == -INFINITY ? 0.0f : R1;
+        l = l * exp2_fast(m - mb) + s.z * exp2_fast(s.x - mb);
+        o = o * exp2_fast(R - rb) + v * exp2_fast(s.y - rb);
         m = m1;
-        if (tid < D) {
-            float acc = 0.0f;
-            const int n = hi - t0 < 128 ? (int)(hi - t0) : 128;
-            for (int j = 0; j < n; j++)
-                acc += s_p[j] * s_vs[j] * (s_at[j] < 0 ? 0.0f : code_value(static_cast<const unsigned char*>(a.p.v)[s_at[j] + tid]));
-            o = o * keep + acc;
-        }
+        R = R1;
     }
-    if (tid < D) {
-        T r;
-        from_float(r, hi > lo ? o / l : 0.0f);
-        static_cast<T*>(a.out)[row * a.o_row + qh * a.o_head + tid] = r;
-    }
-    if (tid == 0 && a.lse) a.lse[(size_t)row * a.q_heads + qh] = hi > lo ? m + logf(l) : -INFINITY;
+    const uint32_t qrow = (uint32_t)r.start + gr / a.group, qh = cut.head * a.group + gr % a.group;
+    store_out<T>(a, qrow, qh, d, l == 0.0f ? 0.0f : o * exp2_fast(R == -INFINITY ? 0.0f : R - m) / l);
+    if (d == 0 && a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
 }  // namespace wm

@@ -4,8 +4,10 @@
 
 namespace wm {
 
+constexpr uint32_t kInjectNoScanner = 1u, kInjectNoCopy = 2u, kInjectNoMeasures = 4u;    // wm_inject_stall
+
 extern thread_local uint32_t g_launches;      // kernels the last call on this thread enqueued
 uint32_t wait_budget_ns();                    // wm_wait_budget_ms
-uint32_t inject_bits();                       // wm_inject_stall: kInject* bits
+uint32_t inject_bits();
 
 }  // namespace wm

@@ -1,0 +1,88 @@
+// Tensor-core building blocks: matrix descriptors, tcgen05.mma and its completion, tensor-memory reads,
+// tiled (tensor-map) copies, and waits bounded by time.  Part of the translation unit wm_pages.cu.
+#pragma once
+
+namespace wm {
+
+// Shared-memory operand descriptor: start, the two strides (bytes) and the swizzle of its rows (2: 128 bytes, 4: 64, 6: 32).
+// K-major tiles (rows of the operand along the swizzled bytes): `stride` is the distance of groups of eight rows.
+// MN-major tiles (the operand's rows run along the swizzled bytes): `stride` is the distance of groups of eight k, `lead` that
+// of blocks of one swizzle width along the rows.
+constexpr uint32_t kSw128 = 2, kSw64 = 4, kSw32 = 6;
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint32_t stride, uint32_t swizzle)
+{
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 | (uint64_t)swizzle << 61;
+}
+// Instruction descriptors: f32 sums of e4m3 x e4m3 (kind f8f6f4) or f16 x f16 (kind f16); mn_a / mn_b: the operand is MN-major.
+__host__ __device__ constexpr uint32_t mma_desc(uint32_t m, uint32_t n, bool mn_a, bool mn_b)
+{
+    return 1u << 4 | (mn_a ? 1u << 15 : 0u) | (mn_b ? 1u << 16 : 0u) | (n >> 3) << 17 | (m >> 4) << 24;
+}
+__device__ __forceinline__ void mma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add) : "memory");
+}
+// An arrival on the barrier when everything this thread has issued so far is done.
+__device__ __forceinline__ void mma_commit(uint32_t bar_s)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar_s) : "memory");
+}
+__device__ __forceinline__ void async_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+template <uint32_t COLS> __device__ __forceinline__ void tmem_alloc(uint32_t smem_result)
+{
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_result), "n"(COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+template <uint32_t COLS> __device__ __forceinline__ void tmem_free(uint32_t taddr)
+{
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "n"(COLS) : "memory");
+}
+// 8 columns of this thread's lane (no wait: tmem_wait_loads before the values are used).
+__device__ __forceinline__ void tmem_read8(uint32_t taddr, float* v)
+{
+    uint32_t* w = reinterpret_cast<uint32_t*>(v);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// One box of a 4-d tensor map into shared memory; rows that lie outside the tensor arrive as zeros.
+__device__ __forceinline__ void tile_load4(uint32_t dst, const void* map, int32_t c1, int32_t c2, int32_t c3, uint32_t bar_s)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"(map), "r"(0), "r"(c1), "r"(c2), "r"(c3), "r"(bar_s) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar_s, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar_s), "r"(bytes) : "memory");
+}
+
+// A wait that gives up after budget_ns.  `dead` is the block's flag in shared memory: once it is up, every wait of the block
+// returns at once, the block runs through to its end on whatever is there and reports the failure.
+__device__ __forceinline__ void mbar_wait(uint32_t bar_s, uint32_t parity, uint32_t budget_ns, volatile uint32_t* dead)
+{
+    if (mbar_try(bar_s, parity)) return;
+    const uint32_t t0 = now_ns();
+    while (!*dead) {
+        if (mbar_try(bar_s, parity)) return;
+        if (now_ns() - t0 > budget_ns) { *dead = 1u; return; }
+    }
+}
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// The largest of the warp's values (NaN only if all are).
+__device__ __forceinline__ float warp_max(float x)
+{
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+}  // namespace wm

@@ -1,9 +1,12 @@
 // The paged 8-bit cache: kernels (sm_100a) and C ABI.
 //   wm_pages_plan    : k_pages_plan
 //   wm_pages_append  : k_pages_append
-//   wm_pages_attend  : k_attend_rows
+//   wm_pages_attend  : k_attend_few -> k_attend_join
 #include <cstdint>
+#include <algorithm>
 #include <cmath>
+#include <mutex>
+#include <type_traits>
 
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -13,6 +16,7 @@
 #include "wm_host.h"
 #include "wm_launch.h"
 #include "wm_pages.cuh"
+#include "wm_mma.cuh"
 #include "wm_attend.cuh"
 
 namespace wm {
@@ -44,12 +48,67 @@ static void append_launch(const AppendArgs& a, cudaStream_t s)
     else launch_after(k_pages_append<T, 128>, grid, 256, 0, s, a);
 }
 
-template <typename T>
-static void attend_launch(const AttendArgs& a, cudaStream_t s)
+// ---- what a device is asked once: its SMs, the kernels' shared memory
+struct PagesDevice {
+    uint32_t sms = 0;
+    bool ready = false;
+};
+static PagesDevice g_pages_dev[64];
+static std::mutex g_pages_mutex;
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static EncodeTiled g_encode_tiled = nullptr;
+
+template <typename T, int D, int RT> static bool few_ready()
 {
-    const dim3 grid(a.n_rows, a.q_heads);
-    if (a.p.head_dim == 64) launch_after(k_attend_rows<T, 64>, grid, 128, 0, s, a);
-    else launch_after(k_attend_rows<T, 128>, grid, 128, 0, s, a);
+    return cudaFuncSetAttribute((const void*)k_attend_few<T, D, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Few<T, D, RT>::kSmem) == cudaSuccess;
+}
+template <typename T, int D> static bool few_ready_all() { return few_ready<T, D, 8>() && few_ready<T, D, 16>() && few_ready<T, D, 32>(); }
+
+static const PagesDevice* pages_device()
+{
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+    std::lock_guard<std::mutex> lock(g_pages_mutex);
+    PagesDevice& d = g_pages_dev[dev];
+    if (d.ready) return &d;
+    if (!g_encode_tiled) {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) return nullptr;
+        g_encode_tiled = (EncodeTiled)f;
+    }
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return nullptr;
+    if (!few_ready_all<__nv_bfloat16, 64>() || !few_ready_all<__nv_bfloat16, 128>() || !few_ready_all<__half, 64>() || !few_ready_all<__half, 128>()) return nullptr;
+    d.sms = (uint32_t)n;
+    d.ready = true;
+    return &d;
+}
+
+// The codes as a tensor of (page, head, token, channel); a box is one page of one head, its rows swizzled as the MMAs read them.
+static bool page_map(CUtensorMap* map, const wm_pages& p, void* codes)
+{
+    const cuuint64_t dims[4] = {p.head_dim, p.page_tokens, p.kv_heads, p.n_pages};
+    const cuuint64_t strides[3] = {p.token_stride, p.kv_heads > 1 ? p.head_stride : p.token_stride, p.n_pages > 1 ? p.page_stride : p.token_stride};
+    const cuuint32_t box[4] = {p.head_dim, p.page_tokens, 1, 1}, step[4] = {1, 1, 1, 1};
+    return g_encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, codes, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          p.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int D, int RT>
+static void few_launch(const AttendArgs& a, const CUtensorMap& k, const CUtensorMap& v, uint32_t workers, cudaStream_t s)
+{
+    launch_after(k_attend_few<T, D, RT>, workers, 160, Few<T, D, RT>::kSmem, s, a, k, v);
+    launch_after(k_attend_join<T, D, RT>, dim3(workers, RT), D, 0, s, a);
+}
+template <typename T, int D>
+static void attend_launch(const AttendArgs& a, const CUtensorMap& k, const CUtensorMap& v, uint32_t workers, uint32_t rows, cudaStream_t s)
+{
+    if (rows <= 8) few_launch<T, D, 8>(a, k, v, workers, s);
+    else if (rows <= 16) few_launch<T, D, 16>(a, k, v, workers, s);
+    else few_launch<T, D, 32>(a, k, v, workers, s);
 }
 
 }  // namespace wm
@@ -97,7 +156,7 @@ wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows
 
 uint64_t wm_pages_workspace_bytes(uint32_t head_dim)
 {
-    return head_dim == 64 || head_dim == 128 ? 1024 : 0;
+    return head_dim == 64 || head_dim == 128 ? attend_workspace() : 0;
 }
 
 wm_status wm_pages_attend(const wm_pages* pages, const int32_t* table, uint32_t table_stride, const int32_t* kv_len,
@@ -116,11 +175,22 @@ wm_status wm_pages_attend(const wm_pages* pages, const int32_t* table, uint32_t 
     if (n_rows == 0) return WM_OK;
     const AttendArgs a = {*pages, shift, table, table_stride, kv_len, q_start, n_requests, q->ptr, out->ptr, q->row_stride, q->head_stride,
                           out->row_stride, out->head_stride, lse, n_rows, q_heads, q_heads / pages->kv_heads, scale,
-                          options & WM_ATTEND_CAUSAL, window, report};
+                          options & WM_ATTEND_CAUSAL, window, static_cast<unsigned char*>(workspace), wait_budget_ns(), inject_bits(), report};
+    const PagesDevice* dev = pages_device();
+    if (!dev) return WM_ERR_CUDA;
+    CUtensorMap k, v;
+    if (!page_map(&k, *pages, pages->k) || !page_map(&v, *pages, pages->v)) return WM_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (type == WM_TYPE_BF16) attend_launch<__nv_bfloat16>(a, s);
-    else attend_launch<__half>(a, s);
-    g_launches = 1;
+    const uint32_t workers = std::min(2u * dev->sms, kMaxWorkers);
+    const uint32_t rows = (uint32_t)std::min((uint64_t)std::min(max_q, n_rows) * a.group, (uint64_t)0xFFFFFFFFu);
+    if (type == WM_TYPE_BF16) {
+        if (pages->head_dim == 64) attend_launch<__nv_bfloat16, 64>(a, k, v, workers, rows, s);
+        else attend_launch<__nv_bfloat16, 128>(a, k, v, workers, rows, s);
+    } else {
+        if (pages->head_dim == 64) attend_launch<__half, 64>(a, k, v, workers, rows, s);
+        else attend_launch<__half, 128>(a, k, v, workers, rows, s);
+    }
+    g_launches = 2;
     return launch_status();
 }
 

@@ -87,13 +87,13 @@ def append(codes, scales, x, slots, page):
 
 def attend(k, v, ks, vs, table, kv_len, q_start, q, scale, causal, window):
     """(out, lse, weight, error): doubles.  k, v, ks, vs: values as the codes and scales stand for.  `weight` is sum p |v| of
-    each output, `reach` the scores' sum |q||k| scale and qmax sum |k| scale, what the error of a score is counted in."""
+    each output, `spread` the largest p times sum |v|, `reach` the scores' sum |q||k| scale and qmax sum |k| scale, what the error of a score is counted in."""
     rows, heads, dim = q.shape
     group = heads // k.shape[1]
     page = k.shape[2]
     out = torch.zeros(rows, heads, dim, dtype=torch.float64)
     lse = torch.full((rows, heads), -math.inf, dtype=torch.float64)
-    weight, reach, floor = torch.zeros_like(out), torch.zeros_like(lse), torch.zeros_like(lse)
+    weight, reach, floor, spread = torch.zeros_like(out), torch.zeros_like(lse), torch.zeros_like(lse), torch.zeros_like(out)
     for i, n in enumerate(kv_len):
         lo, hi = q_start[i], q_start[i + 1]
         if hi == lo:
@@ -115,21 +115,25 @@ def attend(k, v, ks, vs, table, kv_len, q_start, q, scale, causal, window):
                 out[at] = w @ vv[a:b, h]
                 lse[at] = torch.logsumexp(s, 1)
                 weight[at] = w @ vv[a:b, h].abs()
+                spread[at] = w.amax(1, keepdim=True) * vv[a:b, h].abs().sum(0)
                 size = kk[a:b, h].abs()
                 reach[at] = (y.abs() @ size.T).amax(1) * abs(scale)
                 floor[at] = y.abs().amax(1) * size.sum(1).amax() * abs(scale)
-    return out, lse, weight, reach, floor
+    return out, lse, weight, reach, floor, spread
 
 
-def bounds(out, lse, weight, reach, floor, dtype, dim):
+def bounds(out, lse, weight, reach, floor, spread, dtype, dim):
     """How far a kernel may be off (out, lse).  A score is a sum of dim products in 32 bits, each addition off by less
     than 2^-23 of the sum of the products' sizes, and a handful of factors (scales, the exponential): (dim + 8) 2^-23
     reach.  The queries are held in pieces on a grid of 2^-18 of their row's largest or finer: 2^-18 floor.  An
     error d of the scores moves the softmax's weights by a factor within 1 +- 2 d.  Weights are held in 11 significant
-    bits or more (half a step: 2^-12, taken twice for the sum of pieces), sums in 32 bits, and the output is rounded once."""
+    bits or more (half a step: 2^-12, taken twice for the sum of pieces), sums in 32 bits, and the output is rounded once.
+    Small weights lie on a grid: three e4m3 pieces of 2^8 p, each of the remainder times 16, end at steps of
+    2^-9 / 16^2 / 2^8 = 2^-25 of the largest weight of the tile, which is not above the row's (twice the true one for errors of
+    the scores): half a step, 2^-26, for every value, whatever its weight."""
     d = (dim + 8) * 2.0 ** -23 * reach + 2.0 ** -18 * floor
     rounding = torch.finfo(dtype).eps / 2
-    far = 2 * (2 * d[..., None] + 2.0 ** -12) * weight
+    far = 2 * (2 * d[..., None] + 2.0 ** -12) * weight + 2.0 ** -25 * spread
     tiny = torch.finfo(dtype).tiny * torch.finfo(dtype).eps
     return far * (1 + rounding) + rounding * out.abs() + tiny, d + 2.0 ** -18 + 2.0 ** -22 * lse.abs()
 
