@@ -525,7 +525,7 @@ wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows
  *   table     [dev] i32[n_requests][table_stride], kv_len [dev] i32[n_requests], q_start [dev] i32[n_requests + 1]
  *   q, out    n_rows rows of q_heads heads of the pool's head_dim, WM_TYPE_BF16 or WM_TYPE_F16; must not overlap
  *   lse       [dev] f32[n_rows][q_heads] or NULL
- *   q_heads   a multiple of kv_heads, at most 64 * kv_heads
+ *   q_heads   a multiple of kv_heads, at most 64 * kv_heads; n_rows * q_heads / kv_heads <= 2^24
  *   max_q     the most rows any request has, as far as the caller knows (1: a step of single tokens).  It
  *             chooses the kernels; requests with more rows are answered all the same, more slowly
  *   options   WM_ATTEND_CAUSAL or 0

@@ -18,6 +18,7 @@ struct AttendArgs {
     uint32_t n_rows, q_heads, group;
     float scale;
     uint32_t causal, window;
+    uint32_t few_rows;          // requests with more rows (times heads that share a key head) are the other kernel's
     unsigned char* ws;
     uint32_t wait_ns, inject;
     wm_pages_report* rep;
@@ -41,6 +42,14 @@ __device__ __forceinline__ Request request_of(const AttendArgs& a, uint32_t i)
     r.kv = a.kv_len[i];
     r.ok = r.start >= 0 && end >= r.start && (uint32_t)end <= a.n_rows && r.kv >= 0 && (uint32_t)r.kv <= (a.table_stride << a.page_shift);
     r.rows = r.ok ? end - r.start : 0;
+    return r;
+}
+
+// (as k_attend_few sees it)
+__device__ __forceinline__ Request few_request_of(const AttendArgs& a, uint32_t i)
+{
+    Request r = request_of(a, i);
+    if ((uint32_t)r.rows > a.few_rows / a.group) r.rows = 0;
     return r;
 }
 
@@ -90,7 +99,7 @@ template <typename T, int D, int RT> struct Few {
     static constexpr uint32_t kSmem = oMisc + (uint32_t)sizeof(Misc) + 1024;
 };
 
-constexpr uint32_t kMaxWorkers = 512, kPartRows = 32;
+constexpr uint32_t kMaxWorkers = 320, kPartRows = 32;
 // A cut unit's description, left by the worker that has its first tile.
 struct Cut {
     uint32_t valid, req, head, rt, last, slot, pad[2];
@@ -154,7 +163,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
     unsigned long long mine = 0, incl = 0;
     if (warp < 4) {
         for (uint32_t i = tid * per; i < min((tid + 1) * per, a.n); i++) {
-            const Request r = request_of(a, i);
+            const Request r = few_request_of(a, i);
             if (!r.ok && blockIdx.x == 0) pages_fault(a.rep, WM_ERR_ARG, i);
             if (r.rows) mine += shape_of<RT>(a, r).tiles;
         }
@@ -180,7 +189,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
         if (at <= t_begin && t_begin < incl) {
             uint32_t i = tid * per;
             for (;; i++) {
-                const Request r = request_of(a, i);
+                const Request r = few_request_of(a, i);
                 const unsigned long long t = r.rows ? shape_of<RT>(a, r).tiles : 0;
                 if (t_begin < at + t) break;
                 at += t;
@@ -203,7 +212,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
             const uint32_t pages = 128u >> a.page_shift;
             uint32_t stage = 0, phase = 0;
             while (t < t_end) {
-                const Request r = request_of(a, req);
+                const Request r = few_request_of(a, req);
                 const UnitShape u = r.rows ? shape_of<RT>(a, r) : UnitShape{0, 0, 1, 0};
                 if (t >= prefix + u.tiles) { prefix += u.tiles; req++; continue; }
                 const unsigned long long off = t - prefix;
@@ -267,7 +276,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                 mma_commit(bar(M.sbar));
             };
             while (t < t_end) {
-                const Request r = request_of(a, req);
+                const Request r = few_request_of(a, req);
                 const UnitShape u = r.rows ? shape_of<RT>(a, r) : UnitShape{0, 0, 1, 0};
                 if (t >= prefix + u.tiles) { prefix += u.tiles; req++; continue; }
                 const unsigned long long off = t - prefix;

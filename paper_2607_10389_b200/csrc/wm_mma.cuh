@@ -14,14 +14,21 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 | (uint64_t)swizzle << 61;
 }
 // Instruction descriptors: f32 sums of e4m3 x e4m3 (kind f8f6f4) or f16 x f16 (kind f16); mn_a / mn_b: the operand is MN-major.
-__host__ __device__ constexpr uint32_t mma_desc(uint32_t m, uint32_t n, bool mn_a, bool mn_b)
+// (e5m2_a: A's elements are e5m2 instead).
+__host__ __device__ constexpr uint32_t mma_desc(uint32_t m, uint32_t n, bool mn_a, bool mn_b, bool e5m2_a = false)
 {
-    return 1u << 4 | (mn_a ? 1u << 15 : 0u) | (mn_b ? 1u << 16 : 0u) | (n >> 3) << 17 | (m >> 4) << 24;
+    return 1u << 4 | (e5m2_a ? 1u << 7 : 0u) | (mn_a ? 1u << 15 : 0u) | (mn_b ? 1u << 16 : 0u) | (n >> 3) << 17 | (m >> 4) << 24;
 }
 __device__ __forceinline__ void mma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add)
 {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add) : "memory");
+}
+// f16 x f16 with A in tensor memory (a row per lane, two elements a column).
+__device__ __forceinline__ void mma_f16_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(desc), "r"((uint32_t)add) : "memory");
 }
 // An arrival on the barrier when everything this thread has issued so far is done.
 __device__ __forceinline__ void mma_commit(uint32_t bar_s)
@@ -46,6 +53,29 @@ __device__ __forceinline__ void tmem_read8(uint32_t taddr, float* v)
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "r"(taddr) : "memory");
 }
+#define WM_R8(w, i) "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]), "=r"(w[i + 4]), "=r"(w[i + 5]), "=r"(w[i + 6]), "=r"(w[i + 7])
+#define WM_I8(w, i) "r"(w[i]), "r"(w[i + 1]), "r"(w[i + 2]), "r"(w[i + 3]), "r"(w[i + 4]), "r"(w[i + 5]), "r"(w[i + 6]), "r"(w[i + 7])
+__device__ __forceinline__ void tmem_read32(uint32_t taddr, float* v)
+{
+    uint32_t* w = reinterpret_cast<uint32_t*>(v);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : WM_R8(w, 0), WM_R8(w, 8), WM_R8(w, 16), WM_R8(w, 24) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_write32(uint32_t taddr, const float* v)
+{
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(v);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 ::"r"(taddr), WM_I8(w, 0), WM_I8(w, 8), WM_I8(w, 16), WM_I8(w, 24) : "memory");
+}
+__device__ __forceinline__ void tmem_write16(uint32_t taddr, const uint32_t* w)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(taddr), WM_I8(w, 0), WM_I8(w, 8) : "memory");
+}
+#undef WM_R8
+#undef WM_I8
 __device__ __forceinline__ void tmem_wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // One box of a 4-d tensor map into shared memory; rows that lie outside the tensor arrive as zeros.
@@ -82,6 +112,33 @@ __device__ __forceinline__ float warp_max(float x)
 {
     float r;
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// Two at a time: a * b + c and a + b.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)),
+        "l"(*reinterpret_cast<unsigned long long*>(&c)));
+    return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+    return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
 

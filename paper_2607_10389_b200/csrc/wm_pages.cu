@@ -1,7 +1,8 @@
 // The paged 8-bit cache: kernels (sm_100a) and C ABI.
 //   wm_pages_plan    : k_pages_plan
 //   wm_pages_append  : k_pages_append
-//   wm_pages_attend  : k_attend_few -> k_attend_join
+//   wm_pages_attend  : k_attend_few -> k_attend_join; in front of them, where requests may have many rows, k_attend_groups ->
+//                      k_attend_many -> k_attend_many_join
 #include <cstdint>
 #include <algorithm>
 #include <cmath>
@@ -18,6 +19,7 @@
 #include "wm_pages.cuh"
 #include "wm_mma.cuh"
 #include "wm_attend.cuh"
+#include "wm_prompt.cuh"
 
 namespace wm {
 
@@ -65,6 +67,11 @@ template <typename T, int D, int RT> static bool few_ready()
 }
 template <typename T, int D> static bool few_ready_all() { return few_ready<T, D, 8>() && few_ready<T, D, 16>() && few_ready<T, D, 32>(); }
 
+template <typename T, int D> static bool many_ready()
+{
+    return cudaFuncSetAttribute((const void*)k_attend_many<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Many<T, D>::kSmem) == cudaSuccess;
+}
+
 static const PagesDevice* pages_device()
 {
     int dev = -1;
@@ -81,6 +88,7 @@ static const PagesDevice* pages_device()
     int n = 0;
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return nullptr;
     if (!few_ready_all<__nv_bfloat16, 64>() || !few_ready_all<__nv_bfloat16, 128>() || !few_ready_all<__half, 64>() || !few_ready_all<__half, 128>()) return nullptr;
+    if (!many_ready<__nv_bfloat16, 64>() || !many_ready<__nv_bfloat16, 128>() || !many_ready<__half, 64>() || !many_ready<__half, 128>()) return nullptr;
     d.sms = (uint32_t)n;
     d.ready = true;
     return &d;
@@ -103,9 +111,21 @@ static void few_launch(const AttendArgs& a, const CUtensorMap& k, const CUtensor
     launch_after(k_attend_few<T, D, RT>, workers, 160, Few<T, D, RT>::kSmem, s, a, k, v);
     launch_after(k_attend_join<T, D, RT>, dim3(workers, RT), D, 0, s, a);
 }
+constexpr uint32_t kFewRows = 64;          // rows of a request and key head up to which the kernel for few rows has them
 template <typename T, int D>
-static void attend_launch(const AttendArgs& a, const CUtensorMap& k, const CUtensorMap& v, uint32_t workers, uint32_t rows, cudaStream_t s)
+static void attend_launch(AttendArgs a, const CUtensorMap& k, const CUtensorMap& v, uint32_t sms, uint32_t rows, cudaStream_t s)
 {
+    g_launches = 2;
+    a.few_rows = 0xFFFFFFFFu;
+    if (rows > kFewRows) {
+        a.few_rows = kFewRows;
+        const uint32_t workers = std::min(sms, kMaxManyWorkers);
+        launch_after(k_attend_groups, 1, 1024, 0, s, a);
+        launch_after(k_attend_many<T, D>, workers, 512, Many<T, D>::kSmem, s, a, k, v);
+        launch_after(k_attend_many_join<T, D>, dim3(workers, kManyRows / 8), D, 0, s, a);
+        g_launches = 5;
+    }
+    const uint32_t workers = std::min(2u * sms, kMaxWorkers);
     if (rows <= 8) few_launch<T, D, 8>(a, k, v, workers, s);
     else if (rows <= 16) few_launch<T, D, 16>(a, k, v, workers, s);
     else few_launch<T, D, 32>(a, k, v, workers, s);
@@ -156,7 +176,7 @@ wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows
 
 uint64_t wm_pages_workspace_bytes(uint32_t head_dim)
 {
-    return head_dim == 64 || head_dim == 128 ? attend_workspace() : 0;
+    return head_dim == 64 || head_dim == 128 ? attend_workspace() + many_workspace() : 0;
 }
 
 wm_status wm_pages_attend(const wm_pages* pages, const int32_t* table, uint32_t table_stride, const int32_t* kv_len,
@@ -170,27 +190,26 @@ wm_status wm_pages_attend(const wm_pages* pages, const int32_t* table, uint32_t 
     if (n_requests == 0 || n_requests > kMaxRequests || table_stride == 0 || (uint64_t)n_requests * table_stride >= (1ull << 31)) return WM_ERR_ARG;
     if ((uint64_t)table_stride << shift >= (1ull << 31) || n_rows >= (1u << 24) || max_q == 0 || !std::isfinite(scale)) return WM_ERR_ARG;
     if (q_heads == 0 || q_heads % pages->kv_heads || q_heads / pages->kv_heads > 64u) return WM_ERR_ARG;
+    if ((uint64_t)n_rows * (q_heads / pages->kv_heads) > (1ull << 24)) return WM_ERR_ARG;
     if (!workspace || !aligned16(workspace) || workspace_bytes < wm_pages_workspace_bytes(pages->head_dim)) return WM_ERR_ARG;
     g_launches = 0;
     if (n_rows == 0) return WM_OK;
     const AttendArgs a = {*pages, shift, table, table_stride, kv_len, q_start, n_requests, q->ptr, out->ptr, q->row_stride, q->head_stride,
                           out->row_stride, out->head_stride, lse, n_rows, q_heads, q_heads / pages->kv_heads, scale,
-                          options & WM_ATTEND_CAUSAL, window, static_cast<unsigned char*>(workspace), wait_budget_ns(), inject_bits(), report};
+                          options & WM_ATTEND_CAUSAL, window, 0u, static_cast<unsigned char*>(workspace), wait_budget_ns(), inject_bits(), report};
     const PagesDevice* dev = pages_device();
     if (!dev) return WM_ERR_CUDA;
     CUtensorMap k, v;
     if (!page_map(&k, *pages, pages->k) || !page_map(&v, *pages, pages->v)) return WM_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const uint32_t workers = std::min(2u * dev->sms, kMaxWorkers);
     const uint32_t rows = (uint32_t)std::min((uint64_t)std::min(max_q, n_rows) * a.group, (uint64_t)0xFFFFFFFFu);
     if (type == WM_TYPE_BF16) {
-        if (pages->head_dim == 64) attend_launch<__nv_bfloat16, 64>(a, k, v, workers, rows, s);
-        else attend_launch<__nv_bfloat16, 128>(a, k, v, workers, rows, s);
+        if (pages->head_dim == 64) attend_launch<__nv_bfloat16, 64>(a, k, v, dev->sms, rows, s);
+        else attend_launch<__nv_bfloat16, 128>(a, k, v, dev->sms, rows, s);
     } else {
-        if (pages->head_dim == 64) attend_launch<__half, 64>(a, k, v, workers, rows, s);
-        else attend_launch<__half, 128>(a, k, v, workers, rows, s);
+        if (pages->head_dim == 64) attend_launch<__half, 64>(a, k, v, dev->sms, rows, s);
+        else attend_launch<__half, 128>(a, k, v, dev->sms, rows, s);
     }
-    g_launches = 2;
     return launch_status();
 }
 

@@ -1,0 +1,664 @@
+// Attention of many rows (prompts, blocks of tokens) over the paged 8-bit cache.  Part of the translation unit wm_pages.cu.
+#pragma once
+
+namespace wm {
+
+// ------------------------------------------------------------------ many rows: bound by the products and the exponentials
+//
+// A block takes 256 rows of one request and key head (rows run over the heads that share the key head first, then over the
+// queries), two tensor-core tiles of 128, and walks the tokens in tiles of 128:
+//   scores   S = Q K^T: e4m3 x e4m3.  The keys go in as they lie; a query is a sum of pieces (e4m3, then e5m2 for the
+//            remainders: 8 bits of a bf16 element in two pieces, 11 of an f16 in three, exact above 2^-17 and 2^-13 of the row's
+//            largest, else off by less than 2^-20 of it), so no key is ever converted, and two 8-bit passes cost what one
+//            16-bit pass would.
+//   outputs  O += P V: f16 x f16 with the weights in tensor memory, over their scores.  Values are converted once per tile
+//            (exact) by a warpgroup of its own, for all 256 rows.
+// One thread has one row: its maximum and sum need no other thread.  As in the kernel for few rows the pages' scales act in f32,
+// the values' as an exponent; O is referred to a maximum R of weighted scores that follows only in jumps of more than 2^7
+// (weights lie in f16 from 2^8 on downwards, so up to 2^15 there is room), which makes rescaling O in tensor memory rare.
+// Work is dealt out as in the kernel for few rows: equal shares of tiles, units cut between workers are joined in order.
+
+template <typename T, int D> struct Many {
+    static constexpr uint32_t kQP = std::is_same<T, __half>::value ? 3 : 2;
+    static constexpr uint32_t kTile8 = 128 * D, kTile16 = 256 * D;
+    static constexpr uint32_t kKS = kQP == 3 && D == 128 ? 2 : 3, kVS = 2, kHS = 2;     // stages: keys, values as codes, values as halves
+    static constexpr uint32_t kRing = 8;                                                // of scales: more than kKS + 1
+    static constexpr uint32_t kSwD = D == 128 ? kSw128 : kSw64;
+    static constexpr uint32_t oK = 2 * kQP * kTile8, oV = oK + kKS * kTile8, oH = oV + kVS * kTile8, oMisc = oH + kHS * kTile16;
+    struct Misc {
+        unsigned long long kfull[kKS], kfree[kKS], vfull[kVS], vfree[kVS], hfull[kHS], hfree[kHS], qfull, sfull[2], pfull[2], ofull[2], fin;
+        float2 scales[kRing][8];        // of the tile's pages: (key scale, log2 of the value scale)
+        uint32_t tmem, dead, nan_seen;
+    };
+    static constexpr uint32_t kSmem = oMisc + (uint32_t)sizeof(Misc) + 1024;
+};
+
+constexpr uint32_t kManyRows = 256, kMaxManyWorkers = 160, kMaxGroups = 70000;
+// A tile of 256 rows of a request; its key heads' tiles stand one behind the other from `base` on.
+struct Group {
+    unsigned long long base;
+    uint32_t req, rt;
+};
+constexpr uint64_t kManyPartFloats = kManyRows * 128 + kManyRows * 4;
+struct ManyWs {                         // behind the workspace of the kernel for few rows
+    unsigned long long* total;          // tiles in all; [1]: groups
+    Cut* cuts;
+    Group* groups;
+    float* parts;
+};
+__host__ __device__ inline uint64_t many_workspace() { return 16 + kMaxManyWorkers * sizeof(Cut) + (uint64_t)kMaxGroups * sizeof(Group) + kMaxManyWorkers * 2 * kManyPartFloats * 4; }
+__device__ __forceinline__ ManyWs many_ws(unsigned char* ws)
+{
+    ManyWs w;
+    unsigned char* p = ws + attend_workspace();
+    w.total = reinterpret_cast<unsigned long long*>(p);
+    w.cuts = reinterpret_cast<Cut*>(p + 16);
+    w.groups = reinterpret_cast<Group*>(w.cuts + kMaxManyWorkers);
+    w.parts = reinterpret_cast<float*>(w.groups + kMaxGroups);
+    return w;
+}
+
+// What the rows at positions pos0 (first) .. pos1 (last) see.
+struct Span {
+    int32_t any_lo, any_hi, all_lo, all_hi;
+};
+__device__ __forceinline__ int32_t sees_from(const AttendArgs& a, int32_t pos) { return a.window ? max(0, pos + 1 - (int32_t)min(a.window, 0x7FFFFFFFu)) : 0; }
+__device__ __forceinline__ int32_t sees_to(const AttendArgs& a, int32_t kv, int32_t pos) { return a.causal ? min(kv, max(0, pos + 1)) : kv; }
+__device__ __forceinline__ Span span_of(const AttendArgs& a, int32_t kv, int32_t pos0, int32_t pos1)
+{
+    return {sees_from(a, pos0), sees_to(a, kv, pos1), sees_from(a, pos1), sees_to(a, kv, pos0)};
+}
+__device__ __forceinline__ uint32_t group_tiles(const AttendArgs& a, const Request& r, uint32_t rt, uint32_t& j0)
+{
+    const uint32_t row0 = rt * kManyRows, row1 = min(row0 + kManyRows, (uint32_t)r.rows * a.group) - 1u;
+    const Span s = span_of(a, r.kv, r.kv - r.rows + (int32_t)(row0 / a.group), r.kv - r.rows + (int32_t)(row1 / a.group));
+    j0 = (uint32_t)s.any_lo / 128u;
+    const uint32_t end = ((uint32_t)s.any_hi + 127u) / 128u;
+    return end > j0 ? end - j0 : 1u;
+}
+
+// The list of groups with their first tiles, in one block.
+__global__ void __launch_bounds__(1024)
+k_attend_groups(AttendArgs a)
+{
+    __shared__ uint32_t s_first[kMaxRequests + 1];
+    __shared__ unsigned long long s_w[32];
+    const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+    grid_dep_wait();
+    grid_dep_launch();
+    const ManyWs w = many_ws(a.ws);
+    auto scan = [&](unsigned long long v, unsigned long long& all) {           // sum of the threads before, and of all
+        unsigned long long incl = v;
+#pragma unroll
+        for (uint32_t d = 1; d < 32; d <<= 1) {
+            const unsigned long long o = __shfl_up_sync(0xFFFFFFFFu, incl, d);
+            if (lane >= d) incl += o;
+        }
+        __syncthreads();
+        if (lane == 31) s_w[warp] = incl;
+        __syncthreads();
+        unsigned long long before = 0;
+        all = 0;
+        for (uint32_t i = 0; i < 32; i++) { if (i < warp) before += s_w[i]; all += s_w[i]; }
+        return before + incl - v;
+    };
+    constexpr uint32_t kPer = (kMaxRequests + 1023u) / 1024u;
+    uint32_t count[kPer], mine = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < kPer; k++) {
+        const uint32_t i = tid * kPer + k;
+        count[k] = 0;
+        if (i < a.n) {
+            const Request r = request_of(a, i);
+            const uint32_t rows = (uint32_t)r.rows * a.group;
+            if ((uint32_t)r.rows > a.few_rows / a.group) count[k] = (rows + kManyRows - 1u) / kManyRows;
+        }
+        mine += count[k];
+    }
+    unsigned long long all;
+    uint32_t at = (uint32_t)scan(mine, all);
+#pragma unroll
+    for (uint32_t k = 0; k < kPer; k++) {
+        const uint32_t i = tid * kPer + k;
+        if (i < a.n) s_first[i] = at;
+        at += count[k];
+    }
+    const uint32_t groups = (uint32_t)min(all, (unsigned long long)kMaxGroups);
+    if (tid == 0) s_first[a.n] = (uint32_t)all;
+    __syncthreads();
+    unsigned long long base = 0;
+    for (uint32_t g0 = 0; g0 < groups; g0 += 1024) {
+        const uint32_t g = g0 + tid;
+        uint32_t req = 0, rt = 0, tiles = 0;
+        if (g < groups) {
+            req = last_not_above(s_first, a.n, g);
+            rt = g - s_first[req];
+            uint32_t j0;
+            tiles = group_tiles(a, request_of(a, req), rt, j0) * a.p.kv_heads;
+        }
+        unsigned long long sum;
+        const unsigned long long before = scan(tiles, sum);
+        if (g < groups) w.groups[g] = Group{base + before, req, rt};
+        base += sum;
+    }
+    if (tid == 0) { w.total[0] = base; w.total[1] = groups; }
+}
+
+__device__ __forceinline__ uint32_t to_e5m2x2(float lo, float hi)
+{
+    uint16_t r;
+    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t from_e5m2x2(uint32_t codes)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(r) : "h"((uint16_t)codes));
+    return r;
+}
+__device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t addr)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+// Where byte `at` of a tile of D-byte rows lies (the copies' and descriptors' swizzle).
+template <int D> __device__ __forceinline__ uint32_t swizzled(uint32_t at) { return at ^ (((at >> 7) & (D == 128 ? 7u : 3u)) << 4); }
+
+// A worker's segments: consecutive tiles of one unit.
+struct Segment {
+    uint32_t req, rt, head, j, count, j0, nt;
+    Request r;
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(512, 1)
+k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap)
+{
+    using F = Many<T, D>;
+    extern __shared__ unsigned char many_smem[];
+    unsigned char* base = many_smem + ((1024u - ((uint32_t)__cvta_generic_to_shared(many_smem) & 1023u)) & 1023u);
+    const uint32_t base_s = (uint32_t)__cvta_generic_to_shared(base);
+    typename F::Misc& M = *reinterpret_cast<typename F::Misc*>(base + F::oMisc);
+    const uint32_t tid = threadIdx.x, lane = tid % 32, warp = warp_uniform(tid / 32), wg = warp / 4;
+    auto bar = [&](const unsigned long long& b) { return (uint32_t)__cvta_generic_to_shared(&b); };
+
+    if (tid == 0) {
+        for (uint32_t s = 0; s < F::kKS; s++) { mbar_init(&M.kfull[s], 1); mbar_init(&M.kfree[s], 1); }
+        for (uint32_t s = 0; s < F::kVS; s++) { mbar_init(&M.vfull[s], 1); mbar_init(&M.vfree[s], 128); }
+        for (uint32_t s = 0; s < F::kHS; s++) { mbar_init(&M.hfull[s], 128); mbar_init(&M.hfree[s], 1); }
+        for (uint32_t s = 0; s < 2; s++) { mbar_init(&M.sfull[s], 2); mbar_init(&M.pfull[s], 128); mbar_init(&M.ofull[s], 1); }
+        mbar_init(&M.qfull, 256);
+        mbar_init(&M.fin, 1);
+        M.dead = 0;
+        M.nan_seen = 0;
+    }
+    if (warp == 12) tmem_alloc<512>((uint32_t)__cvta_generic_to_shared(&M.tmem));
+    grid_dep_wait();
+    grid_dep_launch();
+    tmem_fence_before_sync();
+    __syncthreads();
+    tmem_fence_after_sync();
+    const uint32_t tmem = M.tmem;
+    const ManyWs W = many_ws(a.ws);
+    const unsigned long long total = W.total[0];
+    const uint32_t groups = (uint32_t)W.total[1];
+    const unsigned long long workers = min((unsigned long long)gridDim.x, total);
+    const unsigned long long t_begin = blockIdx.x < workers ? blockIdx.x * total / workers : total;
+    const unsigned long long t_end = blockIdx.x < workers ? (blockIdx.x + 1ull) * total / workers : total;
+    if (tid == 0) {
+        Cut none = {};
+        W.cuts[blockIdx.x] = none;
+    }
+    // the segment that starts at tile t, group g being the one before or that of t
+    auto segment_at = [&](unsigned long long t, uint32_t& g) {
+        while (g + 1 < groups && W.groups[g + 1].base <= t) g++;
+        const Group G = W.groups[g];
+        Segment s;
+        s.req = G.req;
+        s.rt = G.rt;
+        s.r = request_of(a, G.req);
+        s.nt = group_tiles(a, s.r, G.rt, s.j0);
+        const unsigned long long off = t - G.base;
+        s.head = (uint32_t)(off / s.nt);
+        s.j = (uint32_t)(off % s.nt);
+        s.count = (uint32_t)min((unsigned long long)(s.nt - s.j), t_end - t);
+        return s;
+    };
+    if (t_begin < t_end) {
+        uint32_t g = 0;
+        {
+            uint32_t lo = 0, hi = groups;
+            while (hi - lo > 1) {
+                const uint32_t mid = (lo + hi) / 2;
+                if (W.groups[mid].base <= t_begin) lo = mid; else hi = mid;
+            }
+            g = lo;
+        }
+        unsigned long long t = t_begin;
+        if (warp == 12) {
+            // ---- copies: a lane per page
+            const uint32_t pages = 128u >> a.page_shift;
+            uint32_t ks = 0, kp = 0, vs = 0, vp = 0, ring = 0;
+            const bool copy = !(a.inject & kInjectNoCopy);
+            while (t < t_end) {
+                const Segment s = segment_at(t, g);
+                const int32_t* row = a.table + (size_t)s.req * a.table_stride;
+                for (uint32_t c = 0; c < s.count; c++) {
+                    const uint32_t first = (s.j0 + s.j + c) * 128u;
+                    const uint32_t tokens = first < (uint32_t)s.r.kv ? min(128u, (uint32_t)s.r.kv - first) : 0u;
+                    const uint32_t n = (tokens + a.p.page_tokens - 1u) >> a.page_shift;
+                    int32_t page = 0;
+                    float2 sc = make_float2(0.0f, 0.0f);
+                    if (lane < n) {
+                        page = row[(first >> a.page_shift) + lane];
+                        if ((uint32_t)page < a.p.n_pages) {
+                            const size_t at = (size_t)page * a.p.kv_heads + s.head;
+                            sc = make_float2(a.p.k_scale[at], log2f(a.p.v_scale[at]));
+                        } else {
+                            sc = make_float2(NAN, 0.0f);
+                            page = 0;
+                            pages_fault(a.rep, WM_ERR_ARG, s.req);
+                        }
+                    }
+                    const uint32_t bytes = (n << a.page_shift) * D;
+                    mbar_wait(bar(M.kfree[ks]), kp ^ 1u, a.wait_ns, &M.dead);
+                    if (lane < pages) M.scales[ring][lane] = sc;
+                    __syncwarp();
+                    if (lane == 0 && (copy || n == 0)) mbar_expect(bar(M.kfull[ks]), bytes);
+                    __syncwarp();
+                    if (lane < n && copy) tile_load4(base_s + F::oK + ks * F::kTile8 + (lane << a.page_shift) * D, &kmap, 0, (int32_t)s.head, page, bar(M.kfull[ks]));
+                    mbar_wait(bar(M.vfree[vs]), vp ^ 1u, a.wait_ns, &M.dead);
+                    __syncwarp();
+                    if (lane == 0 && (copy || n == 0)) mbar_expect(bar(M.vfull[vs]), bytes);
+                    __syncwarp();
+                    if (lane < n && copy) tile_load4(base_s + F::oV + vs * F::kTile8 + (lane << a.page_shift) * D, &vmap, 0, (int32_t)s.head, page, bar(M.vfull[vs]));
+                    ring = (ring + 1u) % F::kRing;
+                    if (++ks == F::kKS) { ks = 0; kp ^= 1u; }
+                    if (++vs == F::kVS) { vs = 0; vp ^= 1u; }
+                }
+                t += s.count;
+            }
+            if (*(volatile uint32_t*)&M.dead && copy) {       // nothing may still be on its way when the block leaves
+                const uint32_t t0 = now_ns();
+                for (uint32_t s = 0; s < F::kKS; s++) while (!mbar_try(bar(M.kfull[s]), s < ks ? kp : kp ^ 1u) && now_ns() - t0 < a.wait_ns) {}
+                for (uint32_t s = 0; s < F::kVS; s++) while (!mbar_try(bar(M.vfull[s]), s < vs ? vp : vp ^ 1u) && now_ns() - t0 < a.wait_ns) {}
+            }
+        } else if (warp == 13) {
+            // ---- the products, issued by one thread
+            uint32_t ks = 0, kp = 0, hs = 0, hp = 0, qp = 0, pp = 0;
+            auto scores = [&](uint32_t w, uint32_t st) {
+#pragma unroll
+                for (uint32_t p = 0; p < F::kQP; p++)
+#pragma unroll
+                    for (uint32_t kk = 0; kk < D / 32; kk++)
+                        mma_f8(tmem + w * 128u, smem_desc(base_s + (w * F::kQP + p) * F::kTile8 + kk * 32u, 16, 8 * D, F::kSwD),
+                               smem_desc(base_s + F::oK + st * F::kTile8 + kk * 32u, 16, 8 * D, F::kSwD),
+                               mma_desc(128, 128, false, false, p > 0), p + kk > 0);
+                mma_commit(bar(M.sfull[w]));
+                mbar_arrive_at(bar(M.sfull[w]));        // (and with it what came with the keys: the scales)
+            };
+            if (lane == 0) {
+                while (t < t_end) {
+                    const Segment s = segment_at(t, g);
+                    mbar_wait(bar(M.qfull), qp, a.wait_ns, &M.dead);
+                    qp ^= 1u;
+                    mbar_wait(bar(M.kfull[ks]), kp, a.wait_ns, &M.dead);
+                    tmem_fence_after_sync();
+                    scores(0, ks);
+                    scores(1, ks);
+                    mma_commit(bar(M.kfree[ks]));
+                    if (++ks == F::kKS) { ks = 0; kp ^= 1u; }
+                    for (uint32_t c = 0; c < s.count; c++) {
+                        mbar_wait(bar(M.hfull[hs]), hp, a.wait_ns, &M.dead);
+#pragma unroll
+                        for (uint32_t w = 0; w < 2; w++) {
+                            mbar_wait(bar(M.pfull[w]), pp, a.wait_ns, &M.dead);
+                            tmem_fence_after_sync();
+#pragma unroll
+                            for (uint32_t kk = 0; kk < 8; kk++)
+                                mma_f16_ta(tmem + 256u + w * 128u, tmem + w * 128u + kk * 8u,
+                                           smem_desc(base_s + F::oH + hs * F::kTile16 + kk * 2048u, 16384, 1024, kSw128),
+                                           mma_desc(128, D, false, true), c + kk > 0);
+                            mma_commit(bar(M.ofull[w]));
+                            if (w == 1) mma_commit(bar(M.hfree[hs]));
+                            if (c + 1 < s.count) {
+                                if (w == 0) mbar_wait(bar(M.kfull[ks]), kp, a.wait_ns, &M.dead);
+                                scores(w, ks);
+                                if (w == 1) {
+                                    mma_commit(bar(M.kfree[ks]));
+                                    if (++ks == F::kKS) { ks = 0; kp ^= 1u; }
+                                }
+                            }
+                        }
+                        pp ^= 1u;
+                        if (++hs == F::kHS) { hs = 0; hp ^= 1u; }
+                    }
+                    t += s.count;
+                }
+                if (*(volatile uint32_t*)&M.dead) {            // what was issued is done before the tensor memory is handed back
+                    mma_commit(bar(M.fin));
+                    const uint32_t t0 = now_ns();
+                    while (!mbar_try(bar(M.fin), 0) && now_ns() - t0 < a.wait_ns) {}
+                }
+            }
+            __syncwarp();
+        } else if (wg == 2) {
+            // ---- values to halves: thread = token
+            const uint32_t tok = tid % 128u;
+            uint32_t vs = 0, vp = 0, hs = 0, hp = 0;
+            while (t < t_end) {
+                const Segment s = segment_at(t, g);
+                const uint32_t row0 = s.rt * kManyRows, row1 = min(row0 + kManyRows, (uint32_t)s.r.rows * a.group) - 1u;
+                const Span sp = span_of(a, s.r.kv, s.r.kv - s.r.rows + (int32_t)(row0 / a.group), s.r.kv - s.r.rows + (int32_t)(row1 / a.group));
+                for (uint32_t c = 0; c < s.count; c++) {
+                    const int32_t at = (int32_t)((s.j0 + s.j + c) * 128u + tok);
+                    // a value that not every row sees must not meet the others' zero weights as NaN: its NaN codes become zeros
+                    // here, and rows that do see one find it again when they are done
+                    const bool all = at >= sp.all_lo && at < sp.all_hi, any = at >= sp.any_lo && at < sp.any_hi;
+                    mbar_wait(bar(M.vfull[vs]), vp, a.wait_ns, &M.dead);
+                    mbar_wait(bar(M.hfree[hs]), hp ^ 1u, a.wait_ns, &M.dead);
+                    const uint32_t in = base_s + F::oV + vs * F::kTile8, out = base_s + F::oH + hs * F::kTile16 + tok * 128u;
+                    uint4 v[D / 16];
+#pragma unroll
+                    for (uint32_t i = 0; i < D / 16; i++) v[i] = lds16(in + swizzled<D>(tok * D + i * 16u));
+                    if (!all) {
+                        uint32_t found = 0;
+#pragma unroll
+                        for (uint32_t i = 0; i < D / 16; i++) {
+                            uint32_t* x = &v[i].x;
+#pragma unroll
+                            for (uint32_t k = 0; k < 4; k++) {
+                                const uint32_t is = __vcmpeq4(x[k] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                                found |= is;
+                                x[k] &= ~is;
+                            }
+                        }
+                        if (found && any) M.nan_seen = 1u;
+                    }
+#pragma unroll
+                    for (uint32_t i = 0; i < D / 16; i++) {
+                        const uint32_t sub = out + (i / 4u) * 16384u, ch = (i % 4u) * 2u, x = tok & 7u;
+                        sts16(sub + ((ch ^ x) << 4), from_e4m3x2(v[i].x), from_e4m3x2(v[i].x >> 16), from_e4m3x2(v[i].y), from_e4m3x2(v[i].y >> 16));
+                        sts16(sub + (((ch + 1u) ^ x) << 4), from_e4m3x2(v[i].z), from_e4m3x2(v[i].z >> 16), from_e4m3x2(v[i].w), from_e4m3x2(v[i].w >> 16));
+                    }
+                    async_proxy_fence();
+                    mbar_arrive_at(bar(M.hfull[hs]));
+                    mbar_arrive_at(bar(M.vfree[vs]));
+                    if (++vs == F::kVS) { vs = 0; vp ^= 1u; }
+                    if (++hs == F::kHS) { hs = 0; hp ^= 1u; }
+                }
+                t += s.count;
+            }
+        } else if (wg < 2) {
+            // ---- softmax: thread = row
+            const uint32_t w = wg, tS = tmem + w * 128u + ((warp % 4u) * 32u << 16), tO = tS + 256u;
+            uint32_t sp = 0, ring = 0;       // phase of sfull[w] (and of ofull[w], one behind)
+            while (t < t_end) {
+                const Segment s = segment_at(t, g);
+                const uint32_t local = w * 128u + tid % 128u, gr = s.rt * kManyRows + local, n_rows = (uint32_t)s.r.rows * a.group;
+                const bool live = gr < n_rows;
+                const uint32_t jq = gr / a.group, qrow = (uint32_t)s.r.start + jq, qh = s.head * a.group + gr % a.group;
+                const int32_t pos = s.r.kv - s.r.rows + (int32_t)jq;
+                const int32_t lo = sees_from(a, pos), hi = sees_to(a, s.r.kv, pos);
+                float f;
+                {
+                    // the query's pieces
+                    uint4 q[D / 8];
+                    const T* src = static_cast<const T*>(a.q) + (size_t)qrow * a.q_row + (size_t)qh * a.q_head;
+#pragma unroll
+                    for (uint32_t i = 0; i < D / 8; i++) q[i] = live ? *reinterpret_cast<const uint4*>(src + i * 8) : make_uint4(0, 0, 0, 0);
+                    float top = 0.0f;
+                    bool fine = true;
+#pragma unroll
+                    for (uint32_t i = 0; i < D / 2; i++) {
+                        const float2 x = unpack2((&q[i / 4].x)[i % 4], T());
+                        top = max3(top, fabsf(x.x), fabsf(x.y));
+                        fine = fine && fabsf(x.x) <= 3.4e38f && fabsf(x.y) <= 3.4e38f;
+                    }
+                    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 127);
+                    float up = __uint_as_float((uint32_t)(127 + 7 - e) << 23);
+                    f = fine ? fabsf(a.scale) * 1.4426950408889634f * __uint_as_float((uint32_t)(127 - 7 + e) << 23) : NAN;
+                    if (a.scale < 0.0f) up = -up;
+                    const uint32_t q0 = base_s + w * F::kQP * F::kTile8;
+#pragma unroll
+                    for (uint32_t i = 0; i < D / 16; i++) {
+                        uint32_t piece[F::kQP][4];
+#pragma unroll
+                        for (uint32_t k = 0; k < 8; k++) {
+                            float2 x = unpack2((&q[2 * i + k / 4].x)[k % 4], T());
+                            x.x *= up;
+                            x.y *= up;
+#pragma unroll
+                            for (uint32_t p = 0; p < F::kQP; p++) {
+                                const uint32_t code = p == 0 ? to_e4m3x2(x.x, x.y) : to_e5m2x2(x.x, x.y);
+                                const uint32_t h = p == 0 ? from_e4m3x2(code) : from_e5m2x2(code);
+                                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                                x.x -= back.x;
+                                x.y -= back.y;
+                                if (k % 2 == 0) piece[p][k / 2] = code; else piece[p][k / 2] |= code << 16;
+                            }
+                        }
+#pragma unroll
+                        for (uint32_t p = 0; p < F::kQP; p++)
+                            sts16(q0 + p * F::kTile8 + swizzled<D>((tid % 128u) * D + i * 16u), piece[p][0], piece[p][1], piece[p][2], piece[p][3]);
+                    }
+                    async_proxy_fence();
+                    mbar_arrive_at(bar(M.qfull));
+                }
+                float m = -INFINITY, l = 0.0f, R = -INFINITY;       // R: what O refers to
+                for (uint32_t c = 0; c < s.count; c++) {
+                    const int32_t t0 = (int32_t)((s.j0 + s.j + c) * 128u);
+                    mbar_wait(bar(M.sfull[w]), sp, a.wait_ns, &M.dead);
+                    tmem_fence_after_sync();
+                    const float2* sc = M.scales[ring];
+                    const bool whole = __all_sync(0xFFFFFFFFu, !live || (t0 >= lo && t0 + 128 <= hi));
+                    // the largest score and the largest weighted score
+                    float mt = -INFINITY, rt = -INFINITY;
+#pragma unroll
+                    for (uint32_t ch = 0; ch < 4; ch++) {
+                        float x[32];
+                        tmem_read32(tS + ch * 32u, x);
+                        tmem_wait_loads();
+                        if (!whole) {
+#pragma unroll
+                            for (int i = 0; i < 32; i++) {
+                                const int32_t col = t0 + (int32_t)ch * 32 + i;
+                                if (!(col >= lo && col < hi)) x[i] = -INFINITY;
+                            }
+                        }
+#pragma unroll
+                        for (uint32_t h = 0; h < 2; h++) {
+                            float top = x[16 * h];
+#pragma unroll
+                            for (uint32_t i = 1; i < 15; i += 2) top = max3(top, x[16 * h + i], x[16 * h + i + 1]);
+                            top = fmaxf(top, x[16 * h + 15]);
+                            const float2 z = sc[(ch * 32u + h * 16u) >> a.page_shift];
+                            const float v = top == -INFINITY ? top : top * (f * z.x);
+                            mt = fmaxf(mt, v);
+                            rt = fmaxf(rt, v + z.y);
+                        }
+                    }
+                    const float m1 = fmaxf(m, mt), mb = m1 == -INFINITY ? 0.0f : m1;
+                    l *= exp2_fast(m - mb);
+                    m = m1;
+                    // O's reference follows only when weights could leave f16's range
+                    const bool jump = rt > R + 7.0f;
+                    if (__any_sync(0xFFFFFFFFu, jump)) {
+                        const float R1 = jump ? rt : R;
+                        const float factor = R == -INFINITY ? 0.0f : exp2_fast(R - R1);
+                        R = R1;
+                        if (c > 0) {
+                            mbar_wait(bar(M.ofull[w]), sp ^ 1u, a.wait_ns, &M.dead);     // the tile before is in O
+                            tmem_fence_after_sync();
+                            for (uint32_t ch = 0; ch < D / 32; ch++) {
+                                float x[32];
+                                tmem_read32(tO + ch * 32u, x);
+                                tmem_wait_loads();
+#pragma unroll
+                                for (int i = 0; i < 32; i++) x[i] *= factor;
+                                tmem_write32(tO + ch * 32u, x);
+                            }
+                            tmem_wait_stores();
+                        }
+                    }
+                    const float Rb = R == -INFINITY ? 0.0f : R;
+                    // where a page's value scale is so far below the others' that the weight times it would vanish from l, l is summed apart
+                    bool apart = false;
+                    for (uint32_t p = 0; p < 128u >> a.page_shift; p++) apart = apart || Rb - sc[p].y - mb > 80.0f;
+                    apart = __any_sync(0xFFFFFFFFu, apart);
+#pragma unroll
+                    for (uint32_t ch = 0; ch < 4; ch++) {
+                        float x[32];
+                        tmem_read32(tS + ch * 32u, x);
+                        tmem_wait_loads();
+                        if (!whole) {
+#pragma unroll
+                            for (int i = 0; i < 32; i++) {
+                                const int32_t col = t0 + (int32_t)ch * 32 + i;
+                                if (!(col >= lo && col < hi)) x[i] = -INFINITY;
+                            }
+                        }
+                        uint32_t pk[16];
+#pragma unroll
+                        for (uint32_t h = 0; h < 2; h++) {
+                            const float2 z = sc[(ch * 32u + h * 16u) >> a.page_shift];
+                            const float fac = f * z.x;
+                            if (apart || (!whole && !(fac > 0.0f))) {
+#pragma unroll
+                                for (uint32_t i = 0; i < 16; i += 2) {
+                                    const float x0 = x[16 * h + i] == -INFINITY ? -INFINITY : x[16 * h + i] * fac;
+                                    const float x1 = x[16 * h + i + 1] == -INFINITY ? -INFINITY : x[16 * h + i + 1] * fac;
+                                    l += exp2_fast(x0 - mb) + exp2_fast(x1 - mb);
+                                    pk[8 * h + i / 2] = pack_half2(exp2_fast(x0 + (z.y - Rb + 8.0f)), exp2_fast(x1 + (z.y - Rb + 8.0f)));
+                                }
+                            } else {
+                                const float2 fac2 = make_float2(fac, fac), off2 = make_float2(z.y - Rb + 8.0f, z.y - Rb + 8.0f);
+                                float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll
+                                for (uint32_t i = 0; i < 16; i += 2) {
+                                    float2 y = fma2(make_float2(x[16 * h + i], x[16 * h + i + 1]), fac2, off2);
+                                    y.x = exp2_fast(y.x);
+                                    y.y = exp2_fast(y.y);
+                                    sum = add2(sum, y);
+                                    pk[8 * h + i / 2] = pack_half2(y.x, y.y);
+                                }
+                                l = fmaf(sum.x + sum.y, exp2_fast(Rb - 8.0f - z.y - mb), l);
+                            }
+                        }
+                        tmem_write16(tS + ch * 16u, pk);
+                    }
+                    tmem_wait_stores();
+                    tmem_fence_before_sync();
+                    mbar_arrive_at(bar(M.pfull[w]));
+                    sp ^= 1u;
+                    ring = (ring + 1u) % F::kRing;
+                }
+                // the end of the unit's part
+                mbar_wait(bar(M.ofull[w]), sp ^ 1u, a.wait_ns, &M.dead);
+                tmem_fence_after_sync();
+                const bool full = s.count == s.nt;
+                const uint32_t slot = t == t_begin ? 0 : 1;
+                const bool dead = *(volatile uint32_t*)&M.dead;
+                const float factor = dead ? NAN : !full ? 1.0f : l == 0.0f ? 0.0f : exp2_fast(R == -INFINITY ? 0.0f : R - 8.0f - m) / l;
+                const bool nan = *(volatile uint32_t*)&M.nan_seen != 0u;
+                const int32_t row1 = (int32_t)min((s.rt + 1u) * kManyRows, n_rows) - 1;
+                const Span span = span_of(a, s.r.kv, s.r.kv - s.r.rows + (int32_t)(s.rt * kManyRows / a.group), s.r.kv - s.r.rows + row1 / (int32_t)a.group);
+                for (uint32_t ch = 0; ch < D / 32; ch++) {
+                    float x[32];
+                    tmem_read32(tO + ch * 32u, x);
+                    tmem_wait_loads();
+                    if (!live) continue;
+#pragma unroll
+                    for (int i = 0; i < 32; i++) x[i] = l == 0.0f && full && !dead ? 0.0f : x[i] * factor;
+                    if (nan) {
+                        // rare: NaN values among the tokens that only some rows see
+                        for (int32_t k = max(lo, (int32_t)((s.j0 + s.j) * 128u)); k < min(hi, (int32_t)((s.j0 + s.j + s.count) * 128u)); k++) {
+                            if (k >= span.all_lo && k < span.all_hi) continue;
+                            const int32_t page = a.table[(size_t)s.req * a.table_stride + (k >> a.page_shift)];
+                            if ((uint32_t)page >= a.p.n_pages) continue;
+                            const unsigned char* v = static_cast<const unsigned char*>(a.p.v) + (size_t)page * a.p.page_stride +
+                                                     (size_t)s.head * a.p.head_stride + (size_t)(k & (int32_t)(a.p.page_tokens - 1u)) * a.p.token_stride + ch * 32u;
+#pragma unroll
+                            for (int i = 0; i < 32; i++)
+                                if ((v[i] & 0x7Fu) == 0x7Fu) x[i] = NAN;
+                        }
+                    }
+                    if (full) {
+                        T* out = static_cast<T*>(a.out) + (size_t)qrow * a.o_row + (size_t)qh * a.o_head + ch * 32u;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            __align__(16) T o[8];
+#pragma unroll
+                            for (int k = 0; k < 8; k++) from_float(o[k], x[i + k]);
+                            *reinterpret_cast<uint4*>(out + i) = *reinterpret_cast<const uint4*>(o);
+                        }
+                    } else {
+                        float* part = W.parts + (size_t)(blockIdx.x * 2u + slot) * kManyPartFloats + local * D + ch * 32u;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(part + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+                    }
+                }
+                tmem_fence_before_sync();
+                if (live) {
+                    if (full) {
+                        if (a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = dead ? NAN : l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+                    } else {
+                        *reinterpret_cast<float4*>(W.parts + (size_t)(blockIdx.x * 2u + slot) * kManyPartFloats + kManyRows * 128 + 4 * local) =
+                            make_float4(m, R - 8.0f, dead ? NAN : l, 0.0f);
+                    }
+                }
+                if (!full && s.j == 0 && tid == 0) {
+                    const unsigned long long last = t + s.nt - 1;
+                    Cut cut = {1u, s.req, s.head, s.rt, (uint32_t)(((last + 1) * workers - 1) / total), slot, {0, 0}};
+                    W.cuts[blockIdx.x] = cut;
+                }
+                t += s.count;
+            }
+        }
+    }
+    __syncthreads();
+    if (tid == 0 && *(volatile uint32_t*)&M.dead) pages_fault(a.rep, WM_ERR_TIMEOUT, 0);
+    if (warp == 12) {
+        tmem_fence_after_sync();
+        tmem_free<512>(tmem);
+    }
+}
+
+// The cut units' parts put together: block (worker, 8 rows).
+template <typename T, int D>
+__global__ void __launch_bounds__(D)
+k_attend_many_join(AttendArgs a)
+{
+    grid_dep_wait();
+    grid_dep_launch();
+    const ManyWs W = many_ws(a.ws);
+    const uint32_t w0 = blockIdx.x, d = threadIdx.x;
+    const Cut cut = W.cuts[w0];
+    if (!cut.valid) return;
+    const Request r = request_of(a, cut.req);
+    for (uint32_t i = blockIdx.y * 8u; i < blockIdx.y * 8u + 8u; i++) {
+        const uint32_t gr = cut.rt * kManyRows + i;
+        if (gr >= (uint32_t)r.rows * a.group) return;
+        float m = -INFINITY, R = -INFINITY, l = 0.0f, o = 0.0f;
+        for (uint32_t w = w0; w <= cut.last; w++) {
+            const float* part = W.parts + (size_t)(w * 2u + (w == w0 ? cut.slot : 0u)) * kManyPartFloats;
+            const float4 s = *reinterpret_cast<const float4*>(part + kManyRows * 128 + 4 * i);
+            const float v = part[i * D + d];
+            const float m1 = fmaxf(m, s.x), R1 = fmaxf(R, s.y), mb = m1 == -INFINITY ? 0.0f : m1, rb = R1 == -INFINITY ? 0.0f : R1;
+            l = l * exp2_fast(m - mb) + s.z * exp2_fast(s.x - mb);
+            o = o * exp2_fast(R - rb) + v * exp2_fast(s.y - rb);
+            m = m1;
+            R = R1;
+        }
+        const uint32_t qrow = (uint32_t)r.start + gr / a.group, qh = cut.head * a.group + gr % a.group;
+        store_out<T>(a, qrow, qh, d, l == 0.0f ? 0.0f : o * exp2_fast(R == -INFINITY ? 0.0f : R - m) / l);
+        if (d == 0 && a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    }
+}
+
+}  // namespace wm
