@@ -19,22 +19,36 @@ __host__ __device__ constexpr uint32_t mma_desc(uint32_t m, uint32_t n, bool mn_
 {
     return 1u << 4 | (e5m2_a ? 1u << 7 : 0u) | (mn_a ? 1u << 15 : 0u) | (mn_b ? 1u << 16 : 0u) | (n >> 3) << 17 | (m >> 4) << 24;
 }
-__device__ __forceinline__ void mma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add)
+// The issuing instructions are executed by a whole warp and take effect in the one lane for which `leader` holds: the code around
+// them stays uniform, so that descriptors live in uniform registers (issued from inside a branch of one lane, every operand is moved
+// there by itself; eight MMAs then took 840 cycles to issue).
+__device__ __forceinline__ void mma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add, bool leader = true)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add), "r"((uint32_t)leader) : "memory");
 }
 // f16 x f16 with A in tensor memory (a row per lane, two elements a column).
-__device__ __forceinline__ void mma_f16_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add)
+__device__ __forceinline__ void mma_f16_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add, bool leader = true)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(desc), "r"((uint32_t)add) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(desc), "r"((uint32_t)add), "r"((uint32_t)leader) : "memory");
 }
 // An arrival on the barrier when everything this thread has issued so far is done.
-__device__ __forceinline__ void mma_commit(uint32_t bar_s)
+__device__ __forceinline__ void mma_commit(uint32_t bar_s, bool leader = true)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar_s) : "memory");
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+                 ::"r"(bar_s), "r"((uint32_t)leader) : "memory");
 }
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+template <uint32_t N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <uint32_t N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ void async_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 template <uint32_t COLS> __device__ __forceinline__ void tmem_alloc(uint32_t smem_result)
@@ -61,13 +75,6 @@ __device__ __forceinline__ void tmem_read32(uint32_t taddr, float* v)
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
                  "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
                  : WM_R8(w, 0), WM_R8(w, 8), WM_R8(w, 16), WM_R8(w, 24) : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tmem_write32(uint32_t taddr, const float* v)
-{
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(v);
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-                 ::"r"(taddr), WM_I8(w, 0), WM_I8(w, 8), WM_I8(w, 16), WM_I8(w, 24) : "memory");
 }
 __device__ __forceinline__ void tmem_write16(uint32_t taddr, const uint32_t* w)
 {
@@ -107,14 +114,12 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-// The largest of the warp's values (NaN only if all are).
-__device__ __forceinline__ float warp_max(float x)
+__device__ __forceinline__ float warp_min(float x)
 {
     float r;
-    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    asm volatile("redux.sync.min.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
     return r;
 }
-
 // Two at a time: a * b + c and a + b.
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
 {
@@ -129,6 +134,14 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
     return *reinterpret_cast<float2*>(&r);
 }
+// The largest of the warp's values (NaN only if all are).
+__device__ __forceinline__ float warp_max(float x)
+{
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float r;

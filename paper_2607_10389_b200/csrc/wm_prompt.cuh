@@ -14,8 +14,9 @@ namespace wm {
 //   outputs  O += P V: f16 x f16 with the weights in tensor memory, over their scores.  Values are converted once per tile
 //            (exact) by a warpgroup of its own, for all 256 rows.
 // One thread has one row: its maximum and sum need no other thread.  As in the kernel for few rows the pages' scales act in f32,
-// the values' as an exponent; O is referred to a maximum R of weighted scores that follows only in jumps of more than 2^7
-// (weights lie in f16 from 2^8 on downwards, so up to 2^15 there is room), which makes rescaling O in tensor memory rare.
+// the values' as an exponent; O is referred to a maximum R of weighted scores that follows only in jumps of more than 2^14
+// (weights lie in f16 from 2 on downwards, so up to 2^15 there is room), which makes rescaling O in tensor memory rare: a warp that does it
+// holds up the other three of its tile for 900 cycles, and with jumps of 2^7 one of them did in every other tile.
 // Work is dealt out as in the kernel for few rows: equal shares of tiles, units cut between workers are joined in order.
 
 template <typename T, int D> struct Many {
@@ -26,13 +27,17 @@ template <typename T, int D> struct Many {
     static constexpr uint32_t kSwD = D == 128 ? kSw128 : kSw64;
     static constexpr uint32_t oK = 2 * kQP * kTile8, oV = oK + kKS * kTile8, oH = oV + kVS * kTile8, oMisc = oH + kHS * kTile16;
     struct Misc {
-        unsigned long long kfull[kKS], kfree[kKS], vfull[kVS], vfree[kVS], hfull[kHS], hfree[kHS], qfull, sfull[2], pfull[2], ofull[2], fin;
-        float2 scales[kRing][8];        // of the tile's pages: (key scale, log2 of the value scale)
-        uint32_t tmem, dead, nan_seen;
+        unsigned long long kfull[kKS], kfree[kKS], vfull[kVS], vfree[kVS], hfull[kHS], hfree[kHS], qfull, sfull[2], pfull[2][3], ofull[2], fin;
+        alignas(16) float2 scales[kRing][8];     // of every 16 tokens: (key scale, log2 of the value scale)
+        float least[kRing];                     // the least of the logarithms
+        float f[256];                           // of every row: |scale| log2(e) / its factor
+        uint32_t tmem, dead, nan_seen, first;
     };
     static constexpr uint32_t kSmem = oMisc + (uint32_t)sizeof(Misc) + 1024;
 };
 
+// A weight of the reference's size is 2^kTop in f16; up to 2^kRoom more fits in (2^15 of 65504), and what is 2^-25 below is lost.
+constexpr float kTop = 1.0f, kRoom = 14.0f;
 constexpr uint32_t kManyRows = 256, kMaxManyWorkers = 160, kMaxGroups = 70000;
 // A tile of 256 rows of a request; its key heads' tiles stand one behind the other from `base` on.
 struct Group {
@@ -175,7 +180,8 @@ struct Segment {
     Request r;
 };
 
-template <typename T, int D>
+// GS: tokens that share a scale (64 where pages have at least as many, else 16).
+template <typename T, int D, int GS>
 __global__ void __launch_bounds__(512, 1)
 k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap)
 {
@@ -191,7 +197,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
         for (uint32_t s = 0; s < F::kKS; s++) { mbar_init(&M.kfull[s], 1); mbar_init(&M.kfree[s], 1); }
         for (uint32_t s = 0; s < F::kVS; s++) { mbar_init(&M.vfull[s], 1); mbar_init(&M.vfree[s], 128); }
         for (uint32_t s = 0; s < F::kHS; s++) { mbar_init(&M.hfull[s], 128); mbar_init(&M.hfree[s], 1); }
-        for (uint32_t s = 0; s < 2; s++) { mbar_init(&M.sfull[s], 2); mbar_init(&M.pfull[s], 128); mbar_init(&M.ofull[s], 1); }
+        for (uint32_t s = 0; s < 2; s++) { mbar_init(&M.sfull[s], 2); mbar_init(&M.pfull[s][0], 128); mbar_init(&M.pfull[s][1], 128); mbar_init(&M.pfull[s][2], 128); mbar_init(&M.ofull[s], 1); }
         mbar_init(&M.qfull, 256);
         mbar_init(&M.fin, 1);
         M.dead = 0;
@@ -214,6 +220,10 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
         Cut none = {};
         W.cuts[blockIdx.x] = none;
     }
+    // the first tile's group: all threads look at once (one after the other, halving, took nine trips to the L2)
+    for (uint32_t i = tid; i < groups; i += 512)
+        if (W.groups[i].base <= t_begin && (i + 1 == groups || t_begin < W.groups[i + 1].base)) M.first = i;
+    __syncthreads();
     // the segment that starts at tile t, group g being the one before or that of t
     auto segment_at = [&](unsigned long long t, uint32_t& g) {
         while (g + 1 < groups && W.groups[g + 1].base <= t) g++;
@@ -230,19 +240,13 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
         return s;
     };
     if (t_begin < t_end) {
-        uint32_t g = 0;
-        {
-            uint32_t lo = 0, hi = groups;
-            while (hi - lo > 1) {
-                const uint32_t mid = (lo + hi) / 2;
-                if (W.groups[mid].base <= t_begin) lo = mid; else hi = mid;
-            }
-            g = lo;
-        }
+        uint32_t g = M.first;
         unsigned long long t = t_begin;
+        // (the softmax threads hold a row of scores each, the others little: 2 x 200 + 2 x 56 = 4 x 128 registers)
+        if (wg == 3) {
+            registers_down<56>();
         if (warp == 12) {
             // ---- copies: a lane per page
-            const uint32_t pages = 128u >> a.page_shift;
             uint32_t ks = 0, kp = 0, vs = 0, vp = 0, ring = 0;
             const bool copy = !(a.inject & kInjectNoCopy);
             while (t < t_end) {
@@ -253,7 +257,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                     const uint32_t tokens = first < (uint32_t)s.r.kv ? min(128u, (uint32_t)s.r.kv - first) : 0u;
                     const uint32_t n = (tokens + a.p.page_tokens - 1u) >> a.page_shift;
                     int32_t page = 0;
-                    float2 sc = make_float2(0.0f, 0.0f);
+                    float2 sc = make_float2(1.0f, 0.0f);                 // (where no page is: any finite one)
                     if (lane < n) {
                         page = row[(first >> a.page_shift) + lane];
                         if ((uint32_t)page < a.p.n_pages) {
@@ -267,7 +271,11 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                     }
                     const uint32_t bytes = (n << a.page_shift) * D;
                     mbar_wait(bar(M.kfree[ks]), kp ^ 1u, a.wait_ns, &M.dead);
-                    if (lane < pages) M.scales[ring][lane] = sc;
+                    const float least = warp_min(lane < n ? sc.y : INFINITY);
+                    sc.x = __shfl_sync(0xFFFFFFFFu, sc.x, lane >> (a.page_shift - 4u));
+                    sc.y = __shfl_sync(0xFFFFFFFFu, sc.y, lane >> (a.page_shift - 4u));
+                    if (lane < 8) M.scales[ring][lane] = sc;
+                    if (lane == 8) M.least[ring] = least;
                     __syncwarp();
                     if (lane == 0 && (copy || n == 0)) mbar_expect(bar(M.kfull[ks]), bytes);
                     __syncwarp();
@@ -289,65 +297,68 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                 for (uint32_t s = 0; s < F::kVS; s++) while (!mbar_try(bar(M.vfull[s]), s < vs ? vp : vp ^ 1u) && now_ns() - t0 < a.wait_ns) {}
             }
         } else if (warp == 13) {
-            // ---- the products, issued by one thread
+            // ---- the products
             uint32_t ks = 0, kp = 0, hs = 0, hp = 0, qp = 0, pp = 0;
+            const bool leader = elect_one();
             auto scores = [&](uint32_t w, uint32_t st) {
+                const uint64_t q0 = smem_desc(base_s + w * F::kQP * F::kTile8, 16, 8 * D, F::kSwD), k0 = smem_desc(base_s + F::oK + st * F::kTile8, 16, 8 * D, F::kSwD);
 #pragma unroll
                 for (uint32_t p = 0; p < F::kQP; p++)
 #pragma unroll
                     for (uint32_t kk = 0; kk < D / 32; kk++)
-                        mma_f8(tmem + w * 128u, smem_desc(base_s + (w * F::kQP + p) * F::kTile8 + kk * 32u, 16, 8 * D, F::kSwD),
-                               smem_desc(base_s + F::oK + st * F::kTile8 + kk * 32u, 16, 8 * D, F::kSwD),
-                               mma_desc(128, 128, false, false, p > 0), p + kk > 0);
-                mma_commit(bar(M.sfull[w]));
-                mbar_arrive_at(bar(M.sfull[w]));        // (and with it what came with the keys: the scales)
+                        mma_f8(tmem + w * 128u, q0 + (p * F::kTile8 + kk * 32u) / 16u, k0 + kk * 32u / 16u, mma_desc(128, 128, false, false, p > 0), p + kk > 0, leader);
+                mma_commit(bar(M.sfull[w]), leader);
+                if (leader) mbar_arrive_at(bar(M.sfull[w]));        // (and with it what came with the keys: the scales)
             };
-            if (lane == 0) {
-                while (t < t_end) {
-                    const Segment s = segment_at(t, g);
-                    mbar_wait(bar(M.qfull), qp, a.wait_ns, &M.dead);
-                    qp ^= 1u;
-                    mbar_wait(bar(M.kfull[ks]), kp, a.wait_ns, &M.dead);
-                    tmem_fence_after_sync();
-                    scores(0, ks);
-                    scores(1, ks);
-                    mma_commit(bar(M.kfree[ks]));
-                    if (++ks == F::kKS) { ks = 0; kp ^= 1u; }
-                    for (uint32_t c = 0; c < s.count; c++) {
-                        mbar_wait(bar(M.hfull[hs]), hp, a.wait_ns, &M.dead);
+            while (t < t_end) {
+                const Segment s = segment_at(t, g);
+                const uint32_t count = warp_uniform(s.count);
+                mbar_wait(bar(M.qfull), qp, a.wait_ns, &M.dead);
+                qp ^= 1u;
+                mbar_wait(bar(M.kfull[ks]), kp, a.wait_ns, &M.dead);
+                tmem_fence_after_sync();
+                scores(0, ks);
+                scores(1, ks);
+                mma_commit(bar(M.kfree[ks]), leader);
+                if (++ks == F::kKS) { ks = 0; kp ^= 1u; }
+                for (uint32_t c = 0; c < count; c++) {
+                    mbar_wait(bar(M.hfull[hs]), hp, a.wait_ns, &M.dead);
+                    const uint64_t v0 = smem_desc(base_s + F::oH + hs * F::kTile16, 16384, 1024, kSw128);
+                    if (c + 1 < count) mbar_wait(bar(M.kfull[ks]), kp, a.wait_ns, &M.dead);
 #pragma unroll
-                        for (uint32_t w = 0; w < 2; w++) {
-                            mbar_wait(bar(M.pfull[w]), pp, a.wait_ns, &M.dead);
-                            tmem_fence_after_sync();
+                    for (uint32_t w = 0; w < 2; w++) {
 #pragma unroll
-                            for (uint32_t kk = 0; kk < 8; kk++)
-                                mma_f16_ta(tmem + 256u + w * 128u, tmem + w * 128u + kk * 8u,
-                                           smem_desc(base_s + F::oH + hs * F::kTile16 + kk * 2048u, 16384, 1024, kSw128),
-                                           mma_desc(128, D, false, true), c + kk > 0);
-                            mma_commit(bar(M.ofull[w]));
-                            if (w == 1) mma_commit(bar(M.hfree[hs]));
-                            if (c + 1 < s.count) {
-                                if (w == 0) mbar_wait(bar(M.kfull[ks]), kp, a.wait_ns, &M.dead);
-                                scores(w, ks);
-                                if (w == 1) {
-                                    mma_commit(bar(M.kfree[ks]));
-                                    if (++ks == F::kKS) { ks = 0; kp ^= 1u; }
-                                }
+                        for (uint32_t kk = 0; kk < 8; kk++) {
+                            if (kk == 0 || kk == 4 || kk == 6) {         // the weights of 64, 32 and 32 tokens
+                                mbar_wait(bar(M.pfull[w][kk ? kk / 2 - 1 : 0]), pp, a.wait_ns, &M.dead);
+                                tmem_fence_after_sync();
+                            }
+                            mma_f16_ta(tmem + 256u + w * 128u, tmem + w * 128u + kk * 8u, v0 + kk * 2048u / 16u, mma_desc(128, D, false, true), c + kk > 0, leader);
+                        }
+                        mma_commit(bar(M.ofull[w]), leader);
+                        if (w == 1) mma_commit(bar(M.hfree[hs]), leader);
+                        if (c + 1 < count) {
+                            scores(w, ks);
+                            if (w == 1) {
+                                mma_commit(bar(M.kfree[ks]), leader);
+                                if (++ks == F::kKS) { ks = 0; kp ^= 1u; }
                             }
                         }
-                        pp ^= 1u;
-                        if (++hs == F::kHS) { hs = 0; hp ^= 1u; }
                     }
-                    t += s.count;
+                    pp ^= 1u;
+                    if (++hs == F::kHS) { hs = 0; hp ^= 1u; }
                 }
-                if (*(volatile uint32_t*)&M.dead) {            // what was issued is done before the tensor memory is handed back
-                    mma_commit(bar(M.fin));
-                    const uint32_t t0 = now_ns();
-                    while (!mbar_try(bar(M.fin), 0) && now_ns() - t0 < a.wait_ns) {}
-                }
+                t += count;
+            }
+            if (*(volatile uint32_t*)&M.dead) {            // what was issued is done before the tensor memory is handed back
+                mma_commit(bar(M.fin), leader);
+                const uint32_t t0 = now_ns();
+                while (!mbar_try(bar(M.fin), 0) && now_ns() - t0 < a.wait_ns) {}
             }
             __syncwarp();
+        }
         } else if (wg == 2) {
+            registers_down<56>();
             // ---- values to halves: thread = token
             const uint32_t tok = tid % 128u;
             uint32_t vs = 0, vp = 0, hs = 0, hp = 0;
@@ -394,189 +405,277 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                 }
                 t += s.count;
             }
-        } else if (wg < 2) {
+        } else {
+            registers_up<200>();
             // ---- softmax: thread = row
             const uint32_t w = wg, tS = tmem + w * 128u + ((warp % 4u) * 32u << 16), tO = tS + 256u;
             uint32_t sp = 0, ring = 0;       // phase of sfull[w] (and of ofull[w], one behind)
             while (t < t_end) {
-                const Segment s = segment_at(t, g);
-                const uint32_t local = w * 128u + tid % 128u, gr = s.rt * kManyRows + local, n_rows = (uint32_t)s.r.rows * a.group;
-                const bool live = gr < n_rows;
-                const uint32_t jq = gr / a.group, qrow = (uint32_t)s.r.start + jq, qh = s.head * a.group + gr % a.group;
-                const int32_t pos = s.r.kv - s.r.rows + (int32_t)jq;
-                const int32_t lo = sees_from(a, pos), hi = sees_to(a, s.r.kv, pos);
-                float f;
+                Segment s = segment_at(t, g);
+                bool live;
+                int32_t lo, hi, t0 = (int32_t)((s.j0 + s.j) * 128u);
                 {
-                    // the query's pieces
-                    uint4 q[D / 8];
-                    const T* src = static_cast<const T*>(a.q) + (size_t)qrow * a.q_row + (size_t)qh * a.q_head;
+                    const uint32_t gr = s.rt * kManyRows + w * 128u + tid % 128u;
+                    live = gr < (uint32_t)s.r.rows * a.group;
+                    const int32_t pos = s.r.kv - s.r.rows + (int32_t)(gr / a.group);
+                    lo = sees_from(a, pos);
+                    hi = sees_to(a, s.r.kv, pos);
+                }
+                {
+                    // the queries' pieces: a warp has its own 32 rows, 8 elements a lane.  (Code that runs once a unit is kept short: unrolled, it
+                    // waits for its instructions, 20 cycles for each of them.)
+                    constexpr uint32_t LPR = D / 8, RPI = 32 / LPR, BATCH = 4;          // lanes a row, rows a load
+                    const uint32_t q0 = base_s + w * F::kQP * F::kTile8, part = lane % LPR;
+#pragma unroll 1
+                    for (uint32_t r0 = 0; r0 < 32; r0 += RPI * BATCH) {
+                        uint4 q[BATCH];
 #pragma unroll
-                    for (uint32_t i = 0; i < D / 8; i++) q[i] = live ? *reinterpret_cast<const uint4*>(src + i * 8) : make_uint4(0, 0, 0, 0);
-                    float top = 0.0f;
-                    bool fine = true;
-#pragma unroll
-                    for (uint32_t i = 0; i < D / 2; i++) {
-                        const float2 x = unpack2((&q[i / 4].x)[i % 4], T());
-                        top = max3(top, fabsf(x.x), fabsf(x.y));
-                        fine = fine && fabsf(x.x) <= 3.4e38f && fabsf(x.y) <= 3.4e38f;
-                    }
-                    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 127);
-                    float up = __uint_as_float((uint32_t)(127 + 7 - e) << 23);
-                    f = fine ? fabsf(a.scale) * 1.4426950408889634f * __uint_as_float((uint32_t)(127 - 7 + e) << 23) : NAN;
-                    if (a.scale < 0.0f) up = -up;
-                    const uint32_t q0 = base_s + w * F::kQP * F::kTile8;
-#pragma unroll
-                    for (uint32_t i = 0; i < D / 16; i++) {
-                        uint32_t piece[F::kQP][4];
-#pragma unroll
-                        for (uint32_t k = 0; k < 8; k++) {
-                            float2 x = unpack2((&q[2 * i + k / 4].x)[k % 4], T());
-                            x.x *= up;
-                            x.y *= up;
-#pragma unroll
-                            for (uint32_t p = 0; p < F::kQP; p++) {
-                                const uint32_t code = p == 0 ? to_e4m3x2(x.x, x.y) : to_e5m2x2(x.x, x.y);
-                                const uint32_t h = p == 0 ? from_e4m3x2(code) : from_e5m2x2(code);
-                                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
-                                x.x -= back.x;
-                                x.y -= back.y;
-                                if (k % 2 == 0) piece[p][k / 2] = code; else piece[p][k / 2] |= code << 16;
-                            }
+                        for (uint32_t k = 0; k < BATCH; k++) {
+                            const uint32_t gr = s.rt * kManyRows + (warp * 32u + r0 + k * RPI + lane / LPR);
+                            const uint32_t jq = gr / a.group, qrow = (uint32_t)s.r.start + jq, qh = s.head * a.group + (gr - jq * a.group);
+                            q[k] = make_uint4(0, 0, 0, 0);
+                            if (gr < (uint32_t)s.r.rows * a.group)
+                                q[k] = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (size_t)qrow * a.q_row + (size_t)qh * a.q_head + part * 8u);
                         }
 #pragma unroll
-                        for (uint32_t p = 0; p < F::kQP; p++)
-                            sts16(q0 + p * F::kTile8 + swizzled<D>((tid % 128u) * D + i * 16u), piece[p][0], piece[p][1], piece[p][2], piece[p][3]);
+                        for (uint32_t k = 0; k < BATCH; k++) {
+                            const uint32_t local = warp * 32u + r0 + k * RPI + lane / LPR;       // (of the unit's 256)
+                            float x[8];
+#pragma unroll
+                            for (uint32_t i = 0; i < 4; i++) {
+                                const float2 v = unpack2((&q[k].x)[i], T());
+                                x[2 * i] = v.x;
+                                x[2 * i + 1] = v.y;
+                            }
+                            uint32_t top = 0;
+#pragma unroll
+                            for (uint32_t i = 0; i < 8; i++) top = max(top, __float_as_uint(fabsf(x[i])));
+#pragma unroll
+                            for (uint32_t d = 1; d < LPR; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+                            // a power of two that brings the row's largest element to 128 .. 256; NaN where the row is not finite
+                            const int e = min(max((int)(top >> 23) - 127, -100), 127);
+                            const bool fine = top < 0x7F800000u;
+                            float up = __uint_as_float((uint32_t)(127 + 7 - e) << 23);
+                            if (a.scale < 0.0f) up = -up;
+                            if (part == 0) M.f[local] = fine ? fabsf(a.scale) * 1.4426950408889634f * __uint_as_float((uint32_t)(127 - 7 + e) << 23) : NAN;
+#pragma unroll
+                            for (uint32_t i = 0; i < 8; i++) x[i] *= up;
+#pragma unroll
+                            for (uint32_t p = 0; p < F::kQP; p++) {
+                                uint32_t word[2];
+#pragma unroll
+                                for (uint32_t i = 0; i < 8; i += 2) {
+                                    const uint32_t code = p == 0 ? to_e4m3x2(x[i], x[i + 1]) : to_e5m2x2(x[i], x[i + 1]);
+                                    const uint32_t h = p == 0 ? from_e4m3x2(code) : from_e5m2x2(code);
+                                    const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                                    x[i] -= back.x;
+                                    x[i + 1] -= back.y;
+                                    if (i % 4 == 0) word[i / 4] = code; else word[i / 4] |= code << 16;
+                                }
+                                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(q0 + p * F::kTile8 + swizzled<D>((local - w * 128u) * D + part * 8u)),
+                                             "r"(word[0]), "r"(word[1]) : "memory");
+                            }
+                        }
                     }
                     async_proxy_fence();
                     mbar_arrive_at(bar(M.qfull));
+                    __syncwarp();
                 }
+                const float f = M.f[tid];
                 float m = -INFINITY, l = 0.0f, R = -INFINITY;       // R: what O refers to
-                for (uint32_t c = 0; c < s.count; c++) {
-                    const int32_t t0 = (int32_t)((s.j0 + s.j + c) * 128u);
+                const uint32_t count = s.count;
+                for (uint32_t c = 0; c < count; c++, t0 += 128) {
+                    auto written = [&](uint32_t part) {
+                        tmem_wait_stores();
+                        tmem_fence_before_sync();
+                        mbar_arrive_at(bar(M.pfull[w][part]));
+                    };
+                    const bool whole = __all_sync(0xFFFFFFFFu, !live || (t0 >= lo && t0 + 128 <= hi));
                     mbar_wait(bar(M.sfull[w]), sp, a.wait_ns, &M.dead);
                     tmem_fence_after_sync();
-                    const float2* sc = M.scales[ring];
-                    const bool whole = __all_sync(0xFFFFFFFFu, !live || (t0 >= lo && t0 + 128 <= hi));
-                    // the largest score and the largest weighted score
-                    float mt = -INFINITY, rt = -INFINITY;
+                    const float least = M.least[ring];
+                    bool rolled;
+                    {
+                        float x[128];
 #pragma unroll
-                    for (uint32_t ch = 0; ch < 4; ch++) {
-                        float x[32];
-                        tmem_read32(tS + ch * 32u, x);
+                        for (uint32_t ch = 0; ch < 4; ch++) tmem_read32(tS + ch * 32u, x + ch * 32u);
+                        constexpr uint32_t NG = 128 / GS;
+                        float2 kept[NG == 2 ? 2 : 1];
+                        if (NG == 2) { kept[0] = M.scales[ring][0]; kept[NG == 2 ? 1 : 0] = M.scales[ring][4]; }
+                        auto scale = [&](uint32_t i) { return NG == 2 ? kept[i % 2 % (NG == 2 ? 2 : 1)] : M.scales[ring][i * (GS / 16)]; };   // of group i
                         tmem_wait_loads();
+                        bool odd = false;       // a factor that is not positive would turn what is masked into NaN
                         if (!whole) {
 #pragma unroll
-                            for (int i = 0; i < 32; i++) {
-                                const int32_t col = t0 + (int32_t)ch * 32 + i;
-                                if (!(col >= lo && col < hi)) x[i] = -INFINITY;
+                            for (uint32_t ch = 0; ch < 4; ch++) {
+                                const int32_t c0 = lo - t0 - (int32_t)(32 * ch), c1 = hi - t0 - (int32_t)(32 * ch);
+                                const uint32_t seen = (c1 <= 0 ? 0u : c1 >= 32 ? 0xFFFFFFFFu : (1u << c1) - 1u) & (c0 <= 0 ? 0xFFFFFFFFu : c0 >= 32 ? 0u : 0xFFFFFFFFu << c0);
+#pragma unroll
+                                for (uint32_t i = 0; i < 32; i++)
+                                    if (!(seen >> i & 1u)) x[32 * ch + i] = -INFINITY;
                             }
+#pragma unroll
+                            for (uint32_t i = 0; i < NG; i++) odd = odd || !(scale(i).x > 0.0f) || a.scale == 0.0f;
                         }
+                        // the largest score and the largest weighted score
+                        float mt = m, rt = -INFINITY;
 #pragma unroll
-                        for (uint32_t h = 0; h < 2; h++) {
-                            float top = x[16 * h];
+                        for (uint32_t i = 0; i < NG; i++) {
+                            const float* y = x + GS * i;
+                            float top[4];
 #pragma unroll
-                            for (uint32_t i = 1; i < 15; i += 2) top = max3(top, x[16 * h + i], x[16 * h + i + 1]);
-                            top = fmaxf(top, x[16 * h + 15]);
-                            const float2 z = sc[(ch * 32u + h * 16u) >> a.page_shift];
-                            const float v = top == -INFINITY ? top : top * (f * z.x);
+                            for (uint32_t k = 0; k < 4; k++) top[k] = fmaxf(y[k], y[4 + k]);
+#pragma unroll
+                            for (uint32_t k = 8; k < GS; k += 8)
+#pragma unroll
+                                for (uint32_t e = 0; e < 4; e++) top[e] = max3(top[e], y[k + 2 * e], y[k + 2 * e + 1]);
+                            const float2 z = scale(i);
+                            const float v = max3(fmaxf(top[0], top[1]), top[2], top[3]) * (z.x * f);
                             mt = fmaxf(mt, v);
                             rt = fmaxf(rt, v + z.y);
                         }
-                    }
-                    const float m1 = fmaxf(m, mt), mb = m1 == -INFINITY ? 0.0f : m1;
-                    l *= exp2_fast(m - mb);
-                    m = m1;
-                    // O's reference follows only when weights could leave f16's range
-                    const bool jump = rt > R + 7.0f;
-                    if (__any_sync(0xFFFFFFFFu, jump)) {
-                        const float R1 = jump ? rt : R;
-                        const float factor = R == -INFINITY ? 0.0f : exp2_fast(R - R1);
-                        R = R1;
-                        if (c > 0) {
-                            mbar_wait(bar(M.ofull[w]), sp ^ 1u, a.wait_ns, &M.dead);     // the tile before is in O
-                            tmem_fence_after_sync();
-                            for (uint32_t ch = 0; ch < D / 32; ch++) {
-                                float x[32];
-                                tmem_read32(tO + ch * 32u, x);
-                                tmem_wait_loads();
+                        // O's reference R follows only when weights could leave f16's range (in the first tile there is no O yet); where a
+                        // page's value scale is so far below the others' that the weight times it would vanish from l, l is summed apart, below
+                        if (c == 0) R = rt;
+                        const float mb = mt == -INFINITY ? 0.0f : mt, Rb = R == -INFINITY ? 0.0f : R;
+                        rolled = __any_sync(0xFFFFFFFFu, odd || rt > R + kRoom || !(Rb - least - mb <= 80.0f));
+                        if (!rolled) {
+                            l *= exp2_fast(m - mb);
+                            m = mt;
+                            float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+                            float2 fac2, off2;
 #pragma unroll
-                                for (int i = 0; i < 32; i++) x[i] *= factor;
-                                tmem_write32(tO + ch * 32u, x);
-                            }
-                            tmem_wait_stores();
-                        }
-                    }
-                    const float Rb = R == -INFINITY ? 0.0f : R;
-                    // where a page's value scale is so far below the others' that the weight times it would vanish from l, l is summed apart
-                    bool apart = false;
-                    for (uint32_t p = 0; p < 128u >> a.page_shift; p++) apart = apart || Rb - sc[p].y - mb > 80.0f;
-                    apart = __any_sync(0xFFFFFFFFu, apart);
+                            for (uint32_t ch = 0; ch < 4; ch++) {
+                                uint32_t pk[16];
 #pragma unroll
-                    for (uint32_t ch = 0; ch < 4; ch++) {
-                        float x[32];
-                        tmem_read32(tS + ch * 32u, x);
-                        tmem_wait_loads();
-                        if (!whole) {
-#pragma unroll
-                            for (int i = 0; i < 32; i++) {
-                                const int32_t col = t0 + (int32_t)ch * 32 + i;
-                                if (!(col >= lo && col < hi)) x[i] = -INFINITY;
-                            }
-                        }
-                        uint32_t pk[16];
-#pragma unroll
-                        for (uint32_t h = 0; h < 2; h++) {
-                            const float2 z = sc[(ch * 32u + h * 16u) >> a.page_shift];
-                            const float fac = f * z.x;
-                            if (apart || (!whole && !(fac > 0.0f))) {
-#pragma unroll
-                                for (uint32_t i = 0; i < 16; i += 2) {
-                                    const float x0 = x[16 * h + i] == -INFINITY ? -INFINITY : x[16 * h + i] * fac;
-                                    const float x1 = x[16 * h + i + 1] == -INFINITY ? -INFINITY : x[16 * h + i + 1] * fac;
-                                    l += exp2_fast(x0 - mb) + exp2_fast(x1 - mb);
-                                    pk[8 * h + i / 2] = pack_half2(exp2_fast(x0 + (z.y - Rb + 8.0f)), exp2_fast(x1 + (z.y - Rb + 8.0f)));
+                                for (uint32_t i = 0; i < 32; i += 2) {
+                                    const uint32_t at = 32 * ch + i;
+                                    if (at % GS == 0) {
+                                        const float2 z = scale(at / GS);
+                                        fac2.x = fac2.y = z.x * f;
+                                        off2.x = off2.y = z.y - Rb + kTop;
+                                    }
+                                    float2 e = fma2(make_float2(x[at], x[at + 1]), fac2, off2);
+                                    e.x = exp2_fast(e.x);
+                                    e.y = exp2_fast(e.y);
+                                    pk[i / 2] = pack_half2(e.x, e.y);
+                                    sum[i / 2 % 2] = at % GS < 4 ? e : add2(sum[i / 2 % 2], e);
+                                    if (ch == 3 && i == 14) written(1);
+                                    if (at % GS == GS - 2) {
+                                        sum[0] = add2(sum[0], sum[1]);
+                                        l = fmaf(sum[0].x + sum[0].y, exp2_fast(-off2.x - mb), l);
+                                    }
                                 }
-                            } else {
-                                const float2 fac2 = make_float2(fac, fac), off2 = make_float2(z.y - Rb + 8.0f, z.y - Rb + 8.0f);
-                                float2 sum = make_float2(0.0f, 0.0f);
+                                tmem_write16(tS + ch * 16u, pk);
+                                if (ch == 2) written(0);           // (the stores before are long done)
+                            }
+                            written(2);
+                        }
+                    }
+                    if (rolled) {
+                        // what the way above cannot do, 32 tokens at a time, read twice
+                        auto scores_of = [&](uint32_t ch, float (&v)[32]) {
+                            tmem_read32(tS + ch * 32u, v);
+                            tmem_wait_loads();
+                            const float f0 = M.scales[ring][2 * ch].x * f, f1 = M.scales[ring][2 * ch + 1].x * f;
+                            const int32_t c0 = t0 + (int32_t)(ch * 32u);
 #pragma unroll
-                                for (uint32_t i = 0; i < 16; i += 2) {
-                                    float2 y = fma2(make_float2(x[16 * h + i], x[16 * h + i + 1]), fac2, off2);
-                                    y.x = exp2_fast(y.x);
-                                    y.y = exp2_fast(y.y);
-                                    sum = add2(sum, y);
-                                    pk[8 * h + i / 2] = pack_half2(y.x, y.y);
+                            for (int i = 0; i < 32; i++) v[i] = whole || (c0 + i >= lo && c0 + i < hi) ? v[i] * (i < 16 ? f0 : f1) : -INFINITY;
+                        };
+                        float mt = m, rt = -INFINITY;
+#pragma unroll 1
+                        for (uint32_t ch = 0; ch < 4; ch++) {
+                            float v[32];
+                            scores_of(ch, v);
+                            float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                            for (int i = 0; i < 32; i++) top[i / 16] = fmaxf(top[i / 16], v[i]);
+                            mt = max3(mt, top[0], top[1]);
+                            rt = max3(rt, top[0] + M.scales[ring][2 * ch].y, top[1] + M.scales[ring][2 * ch + 1].y);
+                        }
+                        const float mb = mt == -INFINITY ? 0.0f : mt;
+                        l *= exp2_fast(m - mb);
+                        m = mt;
+                        if (c == 0) R = -INFINITY;
+                        const bool jump = rt > R + kRoom;
+                        if (__any_sync(0xFFFFFFFFu, jump)) {
+                            const float R1 = jump ? rt : R;
+                            const float factor = R == -INFINITY ? 0.0f : exp2_fast(R - R1);
+                            R = R1;
+                            if (c > 0) {
+                                mbar_wait(bar(M.ofull[w]), sp ^ 1u, a.wait_ns, &M.dead);     // the tile before is in O
+                                tmem_fence_after_sync();
+#pragma unroll 1
+                                for (uint32_t ch = 0; ch < D / 32; ch++) {
+                                    float o[32];
+                                    tmem_read32(tO + ch * 32u, o);
+                                    tmem_wait_loads();
+#pragma unroll
+                                    for (int i = 0; i < 32; i++) o[i] *= factor;
+                                    tmem_write16(tO + ch * 32u, reinterpret_cast<const uint32_t*>(o));
+                                    tmem_write16(tO + ch * 32u + 16u, reinterpret_cast<const uint32_t*>(o) + 16);
                                 }
-                                l = fmaf(sum.x + sum.y, exp2_fast(Rb - 8.0f - z.y - mb), l);
                             }
                         }
-                        tmem_write16(tS + ch * 16u, pk);
+                        const float Rb = R == -INFINITY ? 0.0f : R;
+                        const bool apart = __any_sync(0xFFFFFFFFu, Rb - least - mb > 80.0f);
+#pragma unroll 1
+                        for (uint32_t ch = 0; ch < 4; ch++) {
+                            float v[32];
+                            uint32_t pk[16];
+                            scores_of(ch, v);
+                            const float lv0 = M.scales[ring][2 * ch].y, lv1 = M.scales[ring][2 * ch + 1].y;
+                            float sum[2] = {0.0f, 0.0f};
+                            if (apart) {
+#pragma unroll
+                                for (int i = 0; i < 32; i++) l += exp2_fast(v[i] - mb);
+                            }
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                const float off = (i < 16 ? lv0 : lv1) - Rb + kTop;
+                                const float y0 = exp2_fast(v[i] + off), y1 = exp2_fast(v[i + 1] + off);
+                                sum[i / 16] += y0 + y1;
+                                pk[i / 2] = pack_half2(y0, y1);
+                            }
+                            if (!apart) l += sum[0] * exp2_fast(Rb - kTop - lv0 - mb) + sum[1] * exp2_fast(Rb - kTop - lv1 - mb);
+                            tmem_write16(tS + ch * 16u, pk);
+                        }
+                        written(0);
+                        mbar_arrive_at(bar(M.pfull[w][1]));
+                        mbar_arrive_at(bar(M.pfull[w][2]));
                     }
-                    tmem_wait_stores();
-                    tmem_fence_before_sync();
-                    mbar_arrive_at(bar(M.pfull[w]));
                     sp ^= 1u;
                     ring = (ring + 1u) % F::kRing;
                 }
-                // the end of the unit's part
+                // the end of the unit's part (what it is about is asked for again: held through the loop it would cost registers there)
                 mbar_wait(bar(M.ofull[w]), sp ^ 1u, a.wait_ns, &M.dead);
                 tmem_fence_after_sync();
+                s = segment_at(t, g);
+                const uint32_t local = w * 128u + tid % 128u, gr = s.rt * kManyRows + local, n_rows = (uint32_t)s.r.rows * a.group;
+                const uint32_t jq = gr / a.group, qrow = (uint32_t)s.r.start + jq, qh = s.head * a.group + gr % a.group;
                 const bool full = s.count == s.nt;
                 const uint32_t slot = t == t_begin ? 0 : 1;
                 const bool dead = *(volatile uint32_t*)&M.dead;
-                const float factor = dead ? NAN : !full ? 1.0f : l == 0.0f ? 0.0f : exp2_fast(R == -INFINITY ? 0.0f : R - 8.0f - m) / l;
+                const float factor = dead ? NAN : !full ? 1.0f : l == 0.0f ? 0.0f : exp2_fast(R == -INFINITY ? 0.0f : R - kTop - m) / l;
                 const bool nan = *(volatile uint32_t*)&M.nan_seen != 0u;
                 const int32_t row1 = (int32_t)min((s.rt + 1u) * kManyRows, n_rows) - 1;
                 const Span span = span_of(a, s.r.kv, s.r.kv - s.r.rows + (int32_t)(s.rt * kManyRows / a.group), s.r.kv - s.r.rows + row1 / (int32_t)a.group);
+                // a warp's rows go through its part of the queries' memory (their products are done), so that whole lines are stored: a row a thread,
+                // every store touched 32 lines
+                const uint32_t st0 = base_s + w * F::kQP * F::kTile8 + (warp % 4u) * 4096u;
+                unsigned char* dst0 = full ? reinterpret_cast<unsigned char*>(static_cast<T*>(a.out) + (size_t)qrow * a.o_row + (size_t)qh * a.o_head)
+                                           : reinterpret_cast<unsigned char*>(W.parts + (size_t)(blockIdx.x * 2u + slot) * kManyPartFloats + local * D);
+                if (!live) dst0 = nullptr;
+#pragma unroll 1
                 for (uint32_t ch = 0; ch < D / 32; ch++) {
                     float x[32];
                     tmem_read32(tO + ch * 32u, x);
                     tmem_wait_loads();
-                    if (!live) continue;
 #pragma unroll
                     for (int i = 0; i < 32; i++) x[i] = l == 0.0f && full && !dead ? 0.0f : x[i] * factor;
-                    if (nan) {
+                    if (nan && live) {
                         // rare: NaN values among the tokens that only some rows see
+#pragma unroll 1
                         for (int32_t k = max(lo, (int32_t)((s.j0 + s.j) * 128u)); k < min(hi, (int32_t)((s.j0 + s.j + s.count) * 128u)); k++) {
                             if (k >= span.all_lo && k < span.all_hi) continue;
                             const int32_t page = a.table[(size_t)s.req * a.table_stride + (k >> a.page_shift)];
@@ -588,20 +687,31 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                                 if ((v[i] & 0x7Fu) == 0x7Fu) x[i] = NAN;
                         }
                     }
+                    const uint32_t pieces = full ? 4 : 8;                // of 16 bytes, of a row
+                    const uint32_t mine = st0 + lane * 128u;
                     if (full) {
-                        T* out = static_cast<T*>(a.out) + (size_t)qrow * a.o_row + (size_t)qh * a.o_head + ch * 32u;
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
+                        for (uint32_t i = 0; i < 4; i++) {
                             __align__(16) T o[8];
 #pragma unroll
-                            for (int k = 0; k < 8; k++) from_float(o[k], x[i + k]);
-                            *reinterpret_cast<uint4*>(out + i) = *reinterpret_cast<const uint4*>(o);
+                            for (uint32_t k = 0; k < 8; k++) from_float(o[k], x[8 * i + k]);
+                            const uint4 v = *reinterpret_cast<const uint4*>(o);
+                            sts16(mine + ((i ^ (lane & 7u)) << 4), v.x, v.y, v.z, v.w);
                         }
                     } else {
-                        float* part = W.parts + (size_t)(blockIdx.x * 2u + slot) * kManyPartFloats + local * D + ch * 32u;
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(part + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+                        for (uint32_t i = 0; i < 8; i++)
+                            sts16(mine + ((i ^ (lane & 7u)) << 4), __float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
                     }
+                    __syncwarp();
+#pragma unroll 4
+                    for (uint32_t r = lane / pieces; r < 32u; r += 32u / pieces) {
+                        const uint32_t i = lane % pieces;
+                        unsigned char* to = reinterpret_cast<unsigned char*>(__shfl_sync(0xFFFFFFFFu, (unsigned long long)dst0, r));
+                        const uint4 v = lds16(st0 + r * 128u + ((i ^ (r & 7u)) << 4));
+                        if (to) *reinterpret_cast<uint4*>(to + ch * pieces * 16u + i * 16u) = v;
+                    }
+                    __syncwarp();
                 }
                 tmem_fence_before_sync();
                 if (live) {
@@ -609,7 +719,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                         if (a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = dead ? NAN : l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
                     } else {
                         *reinterpret_cast<float4*>(W.parts + (size_t)(blockIdx.x * 2u + slot) * kManyPartFloats + kManyRows * 128 + 4 * local) =
-                            make_float4(m, R - 8.0f, dead ? NAN : l, 0.0f);
+                            make_float4(m, R - kTop, dead ? NAN : l, 0.0f);
                     }
                 }
                 if (!full && s.j == 0 && tid == 0) {
