@@ -13,7 +13,8 @@ namespace wm {
 //            16-bit pass would.
 //   outputs  O += P V: f16 x f16 with the weights in tensor memory, over their scores.  Values are converted once per tile
 //            (exact) by a warpgroup of its own, for all 256 rows.
-// One thread has one row: its maximum and sum need no other thread.  As in the kernel for few rows the pages' scales act in f32,
+// Two threads have one row, 64 of a tile's tokens each (one thread a row left every scheduler with two warps at work, which waited for
+// their own results most of the time).  They have to agree only where O's reference moves; sums meet at the end.  As in the kernel for few rows the pages' scales act in f32,
 // the values' as an exponent; O is referred to a maximum R of weighted scores that follows only in jumps of more than 2^14
 // (weights lie in f16 from 2 on downwards, so up to 2^15 there is room), which makes rescaling O in tensor memory rare: a warp that does it
 // holds up the other three of its tile for 900 cycles, and with jumps of 2^7 one of them did in every other tile.
@@ -22,15 +23,17 @@ namespace wm {
 template <typename T, int D> struct Many {
     static constexpr uint32_t kQP = std::is_same<T, __half>::value ? 3 : 2;
     static constexpr uint32_t kTile8 = 128 * D, kTile16 = 256 * D;
-    static constexpr uint32_t kKS = kQP == 3 && D == 128 ? 2 : 3, kVS = 2, kHS = 2;     // stages: keys, values as codes, values as halves
+    static constexpr uint32_t kKS = kQP == 3 && D == 128 ? 2 : 3, kVS = kQP == 3 && D == 128 ? 1 : 2, kHS = 2;     // stages: keys, values as codes, as halves
     static constexpr uint32_t kRing = 8;                                                // of scales: more than kKS + 1
     static constexpr uint32_t kSwD = D == 128 ? kSw128 : kSw64;
-    static constexpr uint32_t oK = 2 * kQP * kTile8, oV = oK + kKS * kTile8, oH = oV + kVS * kTile8, oMisc = oH + kHS * kTile16;
+    static constexpr uint32_t kQ = kQP * kTile8 > 32768 ? kQP * kTile8 : 32768;         // of 128 rows: the queries' pieces, then the outputs on their way
+    static constexpr uint32_t oK = 2 * kQ, oV = oK + kKS * kTile8, oH = oV + kVS * kTile8, oMisc = oH + kHS * kTile16;
     struct Misc {
-        unsigned long long kfull[kKS], kfree[kKS], vfull[kVS], vfree[kVS], hfull[kHS], hfree[kHS], qfull, sfull[2], pfull[2][3], ofull[2], fin;
+        unsigned long long kfull[kKS], kfree[kKS], vfull[kVS], vfree[kVS], hfull[kHS], hfree[kHS], qfull, sfull[2], pfull[2][4], ofull[2], fin;
         alignas(16) float2 scales[kRing][8];     // of every 16 tokens: (key scale, log2 of the value scale)
         float least[kRing];                     // the least of the logarithms
         float f[256];                           // of every row: |scale| log2(e) / its factor
+        float2 other[2][2][128];                // what the two halves of a row tell each other
         uint32_t tmem, dead, nan_seen, first;
     };
     static constexpr uint32_t kSmem = oMisc + (uint32_t)sizeof(Misc) + 1024;
@@ -182,7 +185,7 @@ struct Segment {
 
 // GS: tokens that share a scale (64 where pages have at least as many, else 16).
 template <typename T, int D, int GS>
-__global__ void __launch_bounds__(512, 1)
+__global__ void __launch_bounds__(640, 1)
 k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap)
 {
     using F = Many<T, D>;
@@ -195,15 +198,15 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
 
     if (tid == 0) {
         for (uint32_t s = 0; s < F::kKS; s++) { mbar_init(&M.kfull[s], 1); mbar_init(&M.kfree[s], 1); }
-        for (uint32_t s = 0; s < F::kVS; s++) { mbar_init(&M.vfull[s], 1); mbar_init(&M.vfree[s], 128); }
-        for (uint32_t s = 0; s < F::kHS; s++) { mbar_init(&M.hfull[s], 128); mbar_init(&M.hfree[s], 1); }
-        for (uint32_t s = 0; s < 2; s++) { mbar_init(&M.sfull[s], 2); mbar_init(&M.pfull[s][0], 128); mbar_init(&M.pfull[s][1], 128); mbar_init(&M.pfull[s][2], 128); mbar_init(&M.ofull[s], 1); }
-        mbar_init(&M.qfull, 256);
+        for (uint32_t s = 0; s < F::kVS; s++) { mbar_init(&M.vfull[s], 1); mbar_init(&M.vfree[s], 64); }
+        for (uint32_t s = 0; s < F::kHS; s++) { mbar_init(&M.hfull[s], 64); mbar_init(&M.hfree[s], 1); }
+        for (uint32_t s = 0; s < 2; s++) { mbar_init(&M.sfull[s], 2); for (uint32_t q = 0; q < 4; q++) mbar_init(&M.pfull[s][q], 128); mbar_init(&M.ofull[s], 1); }
+        mbar_init(&M.qfull, 512);
         mbar_init(&M.fin, 1);
         M.dead = 0;
         M.nan_seen = 0;
     }
-    if (warp == 12) tmem_alloc<512>((uint32_t)__cvta_generic_to_shared(&M.tmem));
+    if (warp == 16) tmem_alloc<512>((uint32_t)__cvta_generic_to_shared(&M.tmem));
     grid_dep_wait();
     grid_dep_launch();
     tmem_fence_before_sync();
@@ -221,7 +224,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
         W.cuts[blockIdx.x] = none;
     }
     // the first tile's group: all threads look at once (one after the other, halving, took nine trips to the L2)
-    for (uint32_t i = tid; i < groups; i += 512)
+    for (uint32_t i = tid; i < groups; i += 640)
         if (W.groups[i].base <= t_begin && (i + 1 == groups || t_begin < W.groups[i + 1].base)) M.first = i;
     __syncthreads();
     // the segment that starts at tile t, group g being the one before or that of t
@@ -242,10 +245,10 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
     if (t_begin < t_end) {
         uint32_t g = M.first;
         unsigned long long t = t_begin;
-        // (the softmax threads hold a row of scores each, the others little: 2 x 200 + 2 x 56 = 4 x 128 registers)
-        if (wg == 3) {
-            registers_down<56>();
-        if (warp == 12) {
+        // (the softmax threads hold half a row of scores each, the others little: 4 x 104 + 64 = 5 x 96 registers)
+        if (wg == 4) {
+            registers_down<64>();
+        if (warp == 16) {
             // ---- copies: a lane per page
             uint32_t ks = 0, kp = 0, vs = 0, vp = 0, ring = 0;
             const bool copy = !(a.inject & kInjectNoCopy);
@@ -296,12 +299,12 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                 for (uint32_t s = 0; s < F::kKS; s++) while (!mbar_try(bar(M.kfull[s]), s < ks ? kp : kp ^ 1u) && now_ns() - t0 < a.wait_ns) {}
                 for (uint32_t s = 0; s < F::kVS; s++) while (!mbar_try(bar(M.vfull[s]), s < vs ? vp : vp ^ 1u) && now_ns() - t0 < a.wait_ns) {}
             }
-        } else if (warp == 13) {
+        } else if (warp == 17) {
             // ---- the products
             uint32_t ks = 0, kp = 0, hs = 0, hp = 0, qp = 0, pp = 0;
             const bool leader = elect_one();
             auto scores = [&](uint32_t w, uint32_t st) {
-                const uint64_t q0 = smem_desc(base_s + w * F::kQP * F::kTile8, 16, 8 * D, F::kSwD), k0 = smem_desc(base_s + F::oK + st * F::kTile8, 16, 8 * D, F::kSwD);
+                const uint64_t q0 = smem_desc(base_s + w * F::kQ, 16, 8 * D, F::kSwD), k0 = smem_desc(base_s + F::oK + st * F::kTile8, 16, 8 * D, F::kSwD);
 #pragma unroll
                 for (uint32_t p = 0; p < F::kQP; p++)
 #pragma unroll
@@ -328,12 +331,15 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
 #pragma unroll
                     for (uint32_t w = 0; w < 2; w++) {
 #pragma unroll
-                        for (uint32_t kk = 0; kk < 8; kk++) {
-                            if (kk == 0 || kk == 4 || kk == 6) {         // the weights of 64, 32 and 32 tokens
-                                mbar_wait(bar(M.pfull[w][kk ? kk / 2 - 1 : 0]), pp, a.wait_ns, &M.dead);
-                                tmem_fence_after_sync();
+                        for (uint32_t q = 0; q < 4; q++) {              // the weights of 32 tokens: of both halves' first, then of their last
+                            mbar_wait(bar(M.pfull[w][q]), pp, a.wait_ns, &M.dead);
+                            tmem_fence_after_sync();
+#pragma unroll
+                            for (uint32_t i = 0; i < 2; i++) {
+                                const uint32_t h = q % 2, kk = 4 * h + 2 * (q / 2) + i;
+                                mma_f16_ta(tmem + 256u + w * 128u, tmem + w * 128u + 64u * h + (kk % 4) * 8u, v0 + kk * 2048u / 16u,
+                                           mma_desc(128, D, false, true), c + q + i > 0, leader);
                             }
-                            mma_f16_ta(tmem + 256u + w * 128u, tmem + w * 128u + kk * 8u, v0 + kk * 2048u / 16u, mma_desc(128, D, false, true), c + kk > 0, leader);
                         }
                         mma_commit(bar(M.ofull[w]), leader);
                         if (w == 1) mma_commit(bar(M.hfree[hs]), leader);
@@ -356,46 +362,46 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                 while (!mbar_try(bar(M.fin), 0) && now_ns() - t0 < a.wait_ns) {}
             }
             __syncwarp();
-        }
-        } else if (wg == 2) {
-            registers_down<56>();
-            // ---- values to halves: thread = token
-            const uint32_t tok = tid % 128u;
+        } else {
+            // ---- values to halves: thread = two tokens
             uint32_t vs = 0, vp = 0, hs = 0, hp = 0;
             while (t < t_end) {
                 const Segment s = segment_at(t, g);
                 const uint32_t row0 = s.rt * kManyRows, row1 = min(row0 + kManyRows, (uint32_t)s.r.rows * a.group) - 1u;
                 const Span sp = span_of(a, s.r.kv, s.r.kv - s.r.rows + (int32_t)(row0 / a.group), s.r.kv - s.r.rows + (int32_t)(row1 / a.group));
                 for (uint32_t c = 0; c < s.count; c++) {
-                    const int32_t at = (int32_t)((s.j0 + s.j + c) * 128u + tok);
                     // a value that not every row sees must not meet the others' zero weights as NaN: its NaN codes become zeros
                     // here, and rows that do see one find it again when they are done
-                    const bool all = at >= sp.all_lo && at < sp.all_hi, any = at >= sp.any_lo && at < sp.any_hi;
                     mbar_wait(bar(M.vfull[vs]), vp, a.wait_ns, &M.dead);
                     mbar_wait(bar(M.hfree[hs]), hp ^ 1u, a.wait_ns, &M.dead);
-                    const uint32_t in = base_s + F::oV + vs * F::kTile8, out = base_s + F::oH + hs * F::kTile16 + tok * 128u;
-                    uint4 v[D / 16];
+#pragma unroll 1
+                    for (uint32_t tok = tid % 64u; tok < 128u; tok += 64u) {
+                        const int32_t at = (int32_t)((s.j0 + s.j + c) * 128u + tok);
+                        const bool all = at >= sp.all_lo && at < sp.all_hi, any = at >= sp.any_lo && at < sp.any_hi;
+                        const uint32_t in = base_s + F::oV + vs * F::kTile8, out = base_s + F::oH + hs * F::kTile16 + tok * 128u;
+                        uint4 v[D / 16];
 #pragma unroll
-                    for (uint32_t i = 0; i < D / 16; i++) v[i] = lds16(in + swizzled<D>(tok * D + i * 16u));
-                    if (!all) {
-                        uint32_t found = 0;
+                        for (uint32_t i = 0; i < D / 16; i++) v[i] = lds16(in + swizzled<D>(tok * D + i * 16u));
+                        if (!all) {
+                            uint32_t found = 0;
+#pragma unroll
+                            for (uint32_t i = 0; i < D / 16; i++) {
+                                uint32_t* x = &v[i].x;
+#pragma unroll
+                                for (uint32_t k = 0; k < 4; k++) {
+                                    const uint32_t is = __vcmpeq4(x[k] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                                    found |= is;
+                                    x[k] &= ~is;
+                                }
+                            }
+                            if (found && any) M.nan_seen = 1u;
+                        }
 #pragma unroll
                         for (uint32_t i = 0; i < D / 16; i++) {
-                            uint32_t* x = &v[i].x;
-#pragma unroll
-                            for (uint32_t k = 0; k < 4; k++) {
-                                const uint32_t is = __vcmpeq4(x[k] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
-                                found |= is;
-                                x[k] &= ~is;
-                            }
+                            const uint32_t sub = out + (i / 4u) * 16384u, ch = (i % 4u) * 2u, x = tok & 7u;
+                            sts16(sub + ((ch ^ x) << 4), from_e4m3x2(v[i].x), from_e4m3x2(v[i].x >> 16), from_e4m3x2(v[i].y), from_e4m3x2(v[i].y >> 16));
+                            sts16(sub + (((ch + 1u) ^ x) << 4), from_e4m3x2(v[i].z), from_e4m3x2(v[i].z >> 16), from_e4m3x2(v[i].w), from_e4m3x2(v[i].w >> 16));
                         }
-                        if (found && any) M.nan_seen = 1u;
-                    }
-#pragma unroll
-                    for (uint32_t i = 0; i < D / 16; i++) {
-                        const uint32_t sub = out + (i / 4u) * 16384u, ch = (i % 4u) * 2u, x = tok & 7u;
-                        sts16(sub + ((ch ^ x) << 4), from_e4m3x2(v[i].x), from_e4m3x2(v[i].x >> 16), from_e4m3x2(v[i].y), from_e4m3x2(v[i].y >> 16));
-                        sts16(sub + (((ch + 1u) ^ x) << 4), from_e4m3x2(v[i].z), from_e4m3x2(v[i].z >> 16), from_e4m3x2(v[i].w), from_e4m3x2(v[i].w >> 16));
                     }
                     async_proxy_fence();
                     mbar_arrive_at(bar(M.hfull[hs]));
@@ -405,33 +411,42 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                 }
                 t += s.count;
             }
+        }
         } else {
-            registers_up<200>();
-            // ---- softmax: thread = row
-            const uint32_t w = wg, tS = tmem + w * 128u + ((warp % 4u) * 32u << 16), tO = tS + 256u;
+            registers_up<104>();
+            // ---- softmax: two threads a row, 64 of a tile's tokens each
+            const uint32_t w = wg / 2u, half = wg % 2u, line = tid % 128u, local = w * 128u + line;       // row of the 128, of the 256
+            const uint32_t tS = tmem + w * 128u + half * 64u + ((warp % 4u) * 32u << 16), tO = tmem + 256u + w * 128u + ((warp % 4u) * 32u << 16);
             uint32_t sp = 0, ring = 0;       // phase of sfull[w] (and of ofull[w], one behind)
+            auto both = [&]() { asm volatile("bar.sync %0, 256;" ::"r"(1u + w) : "memory"); };      // the row's two threads (and the tile's others)
+            auto either = [&](bool v) {
+                uint32_t r;
+                asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                             : "=r"(r) : "r"((uint32_t)v), "r"(1u + w) : "memory");
+                return r != 0u;
+            };
             while (t < t_end) {
                 Segment s = segment_at(t, g);
                 bool live;
-                int32_t lo, hi, t0 = (int32_t)((s.j0 + s.j) * 128u);
+                int32_t lo, hi, t0 = (int32_t)((s.j0 + s.j) * 128u + half * 64u);        // (of this thread's tokens)
                 {
-                    const uint32_t gr = s.rt * kManyRows + w * 128u + tid % 128u;
+                    const uint32_t gr = s.rt * kManyRows + local;
                     live = gr < (uint32_t)s.r.rows * a.group;
                     const int32_t pos = s.r.kv - s.r.rows + (int32_t)(gr / a.group);
                     lo = sees_from(a, pos);
                     hi = sees_to(a, s.r.kv, pos);
                 }
                 {
-                    // the queries' pieces: a warp has its own 32 rows, 8 elements a lane.  (Code that runs once a unit is kept short: unrolled, it
+                    // the queries' pieces: a warp has 16 rows, 8 elements a lane.  (Code that runs once a unit is kept short: unrolled, it
                     // waits for its instructions, 20 cycles for each of them.)
                     constexpr uint32_t LPR = D / 8, RPI = 32 / LPR, BATCH = 4;          // lanes a row, rows a load
-                    const uint32_t q0 = base_s + w * F::kQP * F::kTile8, part = lane % LPR;
+                    const uint32_t q0 = base_s + w * F::kQ, part = lane % LPR;
 #pragma unroll 1
-                    for (uint32_t r0 = 0; r0 < 32; r0 += RPI * BATCH) {
+                    for (uint32_t r0 = 0; r0 < 16; r0 += RPI * BATCH) {
                         uint4 q[BATCH];
 #pragma unroll
                         for (uint32_t k = 0; k < BATCH; k++) {
-                            const uint32_t gr = s.rt * kManyRows + (warp * 32u + r0 + k * RPI + lane / LPR);
+                            const uint32_t gr = s.rt * kManyRows + (warp * 16u + r0 + k * RPI + lane / LPR);
                             const uint32_t jq = gr / a.group, qrow = (uint32_t)s.r.start + jq, qh = s.head * a.group + (gr - jq * a.group);
                             q[k] = make_uint4(0, 0, 0, 0);
                             if (gr < (uint32_t)s.r.rows * a.group)
@@ -439,7 +454,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                         }
 #pragma unroll
                         for (uint32_t k = 0; k < BATCH; k++) {
-                            const uint32_t local = warp * 32u + r0 + k * RPI + lane / LPR;       // (of the unit's 256)
+                            const uint32_t row = warp * 16u + r0 + k * RPI + lane / LPR;       // (of the unit's 256)
                             float x[8];
 #pragma unroll
                             for (uint32_t i = 0; i < 4; i++) {
@@ -457,7 +472,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                             const bool fine = top < 0x7F800000u;
                             float up = __uint_as_float((uint32_t)(127 + 7 - e) << 23);
                             if (a.scale < 0.0f) up = -up;
-                            if (part == 0) M.f[local] = fine ? fabsf(a.scale) * 1.4426950408889634f * __uint_as_float((uint32_t)(127 - 7 + e) << 23) : NAN;
+                            if (part == 0) M.f[row] = fine ? fabsf(a.scale) * 1.4426950408889634f * __uint_as_float((uint32_t)(127 - 7 + e) << 23) : NAN;
 #pragma unroll
                             for (uint32_t i = 0; i < 8; i++) x[i] *= up;
 #pragma unroll
@@ -472,42 +487,42 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                                     x[i + 1] -= back.y;
                                     if (i % 4 == 0) word[i / 4] = code; else word[i / 4] |= code << 16;
                                 }
-                                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(q0 + p * F::kTile8 + swizzled<D>((local - w * 128u) * D + part * 8u)),
+                                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(q0 + p * F::kTile8 + swizzled<D>((row - w * 128u) * D + part * 8u)),
                                              "r"(word[0]), "r"(word[1]) : "memory");
                             }
                         }
                     }
                     async_proxy_fence();
                     mbar_arrive_at(bar(M.qfull));
-                    __syncwarp();
+                    both();
                 }
-                const float f = M.f[tid];
+                const float f = M.f[local];
                 float m = -INFINITY, l = 0.0f, R = -INFINITY;       // R: what O refers to
                 const uint32_t count = s.count;
                 for (uint32_t c = 0; c < count; c++, t0 += 128) {
                     auto written = [&](uint32_t part) {
                         tmem_wait_stores();
                         tmem_fence_before_sync();
-                        mbar_arrive_at(bar(M.pfull[w][part]));
+                        mbar_arrive_at(bar(M.pfull[w][2u * part + half]));
                     };
-                    const bool whole = __all_sync(0xFFFFFFFFu, !live || (t0 >= lo && t0 + 128 <= hi));
+                    const bool whole = __all_sync(0xFFFFFFFFu, !live || (t0 >= lo && t0 + 64 <= hi));
                     mbar_wait(bar(M.sfull[w]), sp, a.wait_ns, &M.dead);
                     tmem_fence_after_sync();
                     const float least = M.least[ring];
+                    constexpr uint32_t NG = 64 / GS;
+                    const float2* scales = &M.scales[ring][half * 4u];
                     bool rolled;
                     {
-                        float x[128];
-#pragma unroll
-                        for (uint32_t ch = 0; ch < 4; ch++) tmem_read32(tS + ch * 32u, x + ch * 32u);
-                        constexpr uint32_t NG = 128 / GS;
-                        float2 kept[NG == 2 ? 2 : 1];
-                        if (NG == 2) { kept[0] = M.scales[ring][0]; kept[NG == 2 ? 1 : 0] = M.scales[ring][4]; }
-                        auto scale = [&](uint32_t i) { return NG == 2 ? kept[i % 2 % (NG == 2 ? 2 : 1)] : M.scales[ring][i * (GS / 16)]; };   // of group i
+                        float x[64];
+                        tmem_read32(tS, x);
+                        tmem_read32(tS + 32u, x + 32);
+                        const float2 first = scales[0];
+                        auto scale = [&](uint32_t i) { return NG == 1 ? first : scales[i * (GS / 16)]; };       // of group i: (key scale, log2 of the value scale)
                         tmem_wait_loads();
                         bool odd = false;       // a factor that is not positive would turn what is masked into NaN
                         if (!whole) {
 #pragma unroll
-                            for (uint32_t ch = 0; ch < 4; ch++) {
+                            for (uint32_t ch = 0; ch < 2; ch++) {
                                 const int32_t c0 = lo - t0 - (int32_t)(32 * ch), c1 = hi - t0 - (int32_t)(32 * ch);
                                 const uint32_t seen = (c1 <= 0 ? 0u : c1 >= 32 ? 0xFFFFFFFFu : (1u << c1) - 1u) & (c0 <= 0 ? 0xFFFFFFFFu : c0 >= 32 ? 0u : 0xFFFFFFFFu << c0);
 #pragma unroll
@@ -534,18 +549,23 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                             mt = fmaxf(mt, v);
                             rt = fmaxf(rt, v + z.y);
                         }
-                        // O's reference R follows only when weights could leave f16's range (in the first tile there is no O yet); where a
-                        // page's value scale is so far below the others' that the weight times it would vanish from l, l is summed apart, below
-                        if (c == 0) R = rt;
-                        const float mb = mt == -INFINITY ? 0.0f : mt, Rb = R == -INFINITY ? 0.0f : R;
-                        rolled = __any_sync(0xFFFFFFFFu, odd || rt > R + kRoom || !(Rb - least - mb <= 80.0f));
+                        // O's reference R, the same in both threads of a row, follows only when weights could leave f16's range (in the first
+                        // tile there is no O yet); where a page's value scale is so far below the others' that the weight times it would
+                        // vanish from l, l is summed apart, below
+                        if (c == 0) {
+                            M.other[w][half][line].x = rt;
+                            both();
+                            R = fmaxf(rt, M.other[w][half ^ 1u][line].x);
+                        }
+                        const float Rb = R == -INFINITY ? 0.0f : R, mb = mt == -INFINITY ? Rb : mt;
+                        rolled = either(odd || rt > R + kRoom || !(Rb - least - mb <= 80.0f));
                         if (!rolled) {
                             l *= exp2_fast(m - mb);
                             m = mt;
                             float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
                             float2 fac2, off2;
 #pragma unroll
-                            for (uint32_t ch = 0; ch < 4; ch++) {
+                            for (uint32_t ch = 0; ch < 2; ch++) {
                                 uint32_t pk[16];
 #pragma unroll
                                 for (uint32_t i = 0; i < 32; i += 2) {
@@ -560,16 +580,15 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                                     e.y = exp2_fast(e.y);
                                     pk[i / 2] = pack_half2(e.x, e.y);
                                     sum[i / 2 % 2] = at % GS < 4 ? e : add2(sum[i / 2 % 2], e);
-                                    if (ch == 3 && i == 14) written(1);
+                                    if (ch == 1 && i == 14) written(0);      // (the stores before are long done)
                                     if (at % GS == GS - 2) {
                                         sum[0] = add2(sum[0], sum[1]);
                                         l = fmaf(sum[0].x + sum[0].y, exp2_fast(-off2.x - mb), l);
                                     }
                                 }
                                 tmem_write16(tS + ch * 16u, pk);
-                                if (ch == 2) written(0);           // (the stores before are long done)
                             }
-                            written(2);
+                            written(1);
                         }
                     }
                     if (rolled) {
@@ -577,36 +596,37 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                         auto scores_of = [&](uint32_t ch, float (&v)[32]) {
                             tmem_read32(tS + ch * 32u, v);
                             tmem_wait_loads();
-                            const float f0 = M.scales[ring][2 * ch].x * f, f1 = M.scales[ring][2 * ch + 1].x * f;
+                            const float f0 = scales[2 * ch].x * f, f1 = scales[2 * ch + 1].x * f;
                             const int32_t c0 = t0 + (int32_t)(ch * 32u);
 #pragma unroll
                             for (int i = 0; i < 32; i++) v[i] = whole || (c0 + i >= lo && c0 + i < hi) ? v[i] * (i < 16 ? f0 : f1) : -INFINITY;
                         };
                         float mt = m, rt = -INFINITY;
 #pragma unroll 1
-                        for (uint32_t ch = 0; ch < 4; ch++) {
+                        for (uint32_t ch = 0; ch < 2; ch++) {
                             float v[32];
                             scores_of(ch, v);
                             float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
                             for (int i = 0; i < 32; i++) top[i / 16] = fmaxf(top[i / 16], v[i]);
                             mt = max3(mt, top[0], top[1]);
-                            rt = max3(rt, top[0] + M.scales[ring][2 * ch].y, top[1] + M.scales[ring][2 * ch + 1].y);
+                            rt = max3(rt, top[0] + scales[2 * ch].y, top[1] + scales[2 * ch + 1].y);
                         }
-                        const float mb = mt == -INFINITY ? 0.0f : mt;
-                        l *= exp2_fast(m - mb);
-                        m = mt;
+                        M.other[w][half][line].x = rt;
+                        both();
+                        rt = fmaxf(rt, M.other[w][half ^ 1u][line].x);
+                        both();                                          // (read, before the next is written)
                         if (c == 0) R = -INFINITY;
                         const bool jump = rt > R + kRoom;
                         if (__any_sync(0xFFFFFFFFu, jump)) {
                             const float R1 = jump ? rt : R;
                             const float factor = R == -INFINITY ? 0.0f : exp2_fast(R - R1);
                             R = R1;
-                            if (c > 0) {
+                            if (c > 0) {                                             // (either thread of a row has half of its channels)
                                 mbar_wait(bar(M.ofull[w]), sp ^ 1u, a.wait_ns, &M.dead);     // the tile before is in O
                                 tmem_fence_after_sync();
 #pragma unroll 1
-                                for (uint32_t ch = 0; ch < D / 32; ch++) {
+                                for (uint32_t ch = half * D / 64u; ch < (half + 1u) * D / 64u; ch++) {
                                     float o[32];
                                     tmem_read32(tO + ch * 32u, o);
                                     tmem_wait_loads();
@@ -617,14 +637,16 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                                 }
                             }
                         }
-                        const float Rb = R == -INFINITY ? 0.0f : R;
-                        const bool apart = __any_sync(0xFFFFFFFFu, Rb - least - mb > 80.0f);
+                        const float Rb = R == -INFINITY ? 0.0f : R, mb = mt == -INFINITY ? Rb : mt;
+                        l *= exp2_fast(m - mb);
+                        m = mt;
+                        const bool apart = __any_sync(0xFFFFFFFFu, !(Rb - least - mb <= 80.0f));
 #pragma unroll 1
-                        for (uint32_t ch = 0; ch < 4; ch++) {
+                        for (uint32_t ch = 0; ch < 2; ch++) {
                             float v[32];
                             uint32_t pk[16];
                             scores_of(ch, v);
-                            const float lv0 = M.scales[ring][2 * ch].y, lv1 = M.scales[ring][2 * ch + 1].y;
+                            const float lv0 = scales[2 * ch].y, lv1 = scales[2 * ch + 1].y;
                             float sum[2] = {0.0f, 0.0f};
                             if (apart) {
 #pragma unroll
@@ -641,8 +663,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                             tmem_write16(tS + ch * 16u, pk);
                         }
                         written(0);
-                        mbar_arrive_at(bar(M.pfull[w][1]));
-                        mbar_arrive_at(bar(M.pfull[w][2]));
+                        mbar_arrive_at(bar(M.pfull[w][2u + half]));
                     }
                     sp ^= 1u;
                     ring = (ring + 1u) % F::kRing;
@@ -651,10 +672,18 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                 mbar_wait(bar(M.ofull[w]), sp ^ 1u, a.wait_ns, &M.dead);
                 tmem_fence_after_sync();
                 s = segment_at(t, g);
-                const uint32_t local = w * 128u + tid % 128u, gr = s.rt * kManyRows + local, n_rows = (uint32_t)s.r.rows * a.group;
+                const uint32_t gr = s.rt * kManyRows + local, n_rows = (uint32_t)s.r.rows * a.group;
                 const uint32_t jq = gr / a.group, qrow = (uint32_t)s.r.start + jq, qh = s.head * a.group + gr % a.group;
                 const bool full = s.count == s.nt;
                 const uint32_t slot = t == t_begin ? 0 : 1;
+                M.other[w][half][line] = make_float2(m, l);          // (behind the votes of the last tile: nobody reads what was there)
+                both();
+                {
+                    const float2 o = M.other[w][half ^ 1u][line];
+                    const float m1 = fmaxf(m, o.x), mb = m1 == -INFINITY ? 0.0f : m1;
+                    l = half ? o.y * exp2_fast(o.x - mb) + l * exp2_fast(m - mb) : l * exp2_fast(m - mb) + o.y * exp2_fast(o.x - mb);
+                    m = m1;
+                }
                 const bool dead = *(volatile uint32_t*)&M.dead;
                 const float factor = dead ? NAN : !full ? 1.0f : l == 0.0f ? 0.0f : exp2_fast(R == -INFINITY ? 0.0f : R - kTop - m) / l;
                 const bool nan = *(volatile uint32_t*)&M.nan_seen != 0u;
@@ -662,12 +691,12 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                 const Span span = span_of(a, s.r.kv, s.r.kv - s.r.rows + (int32_t)(s.rt * kManyRows / a.group), s.r.kv - s.r.rows + row1 / (int32_t)a.group);
                 // a warp's rows go through its part of the queries' memory (their products are done), so that whole lines are stored: a row a thread,
                 // every store touched 32 lines
-                const uint32_t st0 = base_s + w * F::kQP * F::kTile8 + (warp % 4u) * 4096u;
+                const uint32_t st0 = base_s + w * F::kQ + (warp % 8u) * 4096u;
                 unsigned char* dst0 = full ? reinterpret_cast<unsigned char*>(static_cast<T*>(a.out) + (size_t)qrow * a.o_row + (size_t)qh * a.o_head)
                                            : reinterpret_cast<unsigned char*>(W.parts + (size_t)(blockIdx.x * 2u + slot) * kManyPartFloats + local * D);
                 if (!live) dst0 = nullptr;
 #pragma unroll 1
-                for (uint32_t ch = 0; ch < D / 32; ch++) {
+                for (uint32_t ch = half * D / 64u; ch < (half + 1u) * D / 64u; ch++) {           // (either thread of a row has half of its channels)
                     float x[32];
                     tmem_read32(tO + ch * 32u, x);
                     tmem_wait_loads();
@@ -714,7 +743,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                     __syncwarp();
                 }
                 tmem_fence_before_sync();
-                if (live) {
+                if (live && half == 0u) {
                     if (full) {
                         if (a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = dead ? NAN : l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
                     } else {
@@ -727,13 +756,14 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                     Cut cut = {1u, s.req, s.head, s.rt, (uint32_t)(((last + 1) * workers - 1) / total), slot, {0, 0}};
                     W.cuts[blockIdx.x] = cut;
                 }
+                both();          // (both halves have read what the other left, and the outputs' way is free)
                 t += s.count;
             }
         }
     }
     __syncthreads();
     if (tid == 0 && *(volatile uint32_t*)&M.dead) pages_fault(a.rep, WM_ERR_TIMEOUT, 0);
-    if (warp == 12) {
+    if (warp == 16) {
         tmem_fence_after_sync();
         tmem_free<512>(tmem);
     }
