@@ -124,7 +124,7 @@ static void attend_launch(AttendArgs a, const CUtensorMap& k, const CUtensorMap&
         const uint32_t workers = std::min(sms, kMaxManyWorkers);
         launch_after(k_attend_groups, 1, 1024, 0, s, a);
         launch_after(a.p.page_tokens >= 64 ? k_attend_many<T, D, 64> : k_attend_many<T, D, 16>, workers, 640, Many<T, D>::kSmem, s, a, k, v);
-        launch_after(k_attend_many_join<T, D>, dim3(workers, kManyRows / 8), D, 0, s, a);
+        launch_after(k_attend_many_join<T, D>, dim3(workers, kManyRows / 8), 2 * D, 0, s, a);
         g_launches = 5;
     }
     const uint32_t workers = std::min(2u * sms, kMaxWorkers);

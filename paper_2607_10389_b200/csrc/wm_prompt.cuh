@@ -20,6 +20,13 @@ namespace wm {
 // holds up the other three of its tile for 900 cycles, and with jumps of 2^7 one of them did in every other tile.
 // Work is dealt out as in the kernel for few rows: equal shares of tiles, units cut between workers are joined in order.
 
+// A worker's segments: consecutive tiles of one unit.  base, end: the first tile of its group's first key head, and behind its last's.
+struct Segment {
+    uint32_t req, rt, head, j, count, j0, nt;
+    Request r;
+    unsigned long long base, end;
+};
+
 template <typename T, int D> struct Many {
     static constexpr uint32_t kQP = std::is_same<T, __half>::value ? 3 : 2;
     static constexpr uint32_t kTile8 = 128 * D, kTile16 = 256 * D;
@@ -29,10 +36,11 @@ template <typename T, int D> struct Many {
     static constexpr uint32_t kQ = kQP * kTile8 > 32768 ? kQP * kTile8 : 32768;         // of 128 rows: the queries' pieces, then the outputs on their way
     static constexpr uint32_t oK = 2 * kQ, oV = oK + kKS * kTile8, oH = oV + kVS * kTile8, oMisc = oH + kHS * kTile16;
     struct Misc {
-        unsigned long long kfull[kKS], kfree[kKS], vfull[kVS], vfree[kVS], hfull[kHS], hfree[kHS], qfull, sfull[2], pfull[2][4], ofull[2], fin;
+        unsigned long long kfull[kKS], kfree[kKS], vfull[kVS], vfree[kVS], hfull[kHS], hfree[kHS], qfull, sfull[2], pfull[2][2], ofull[2], fin;
         alignas(16) float2 scales[kRing][8];     // of every 16 tokens: (key scale, log2 of the value scale)
         float least[kRing];                     // the least of the logarithms
         float f[256];                           // of every row: |scale| log2(e) / its factor
+        Segment seg[2];                         // what the two tiles' softmax threads are at
         float2 other[2][2][128];                // what the two halves of a row tell each other
         uint32_t tmem, dead, nan_seen, first;
     };
@@ -177,12 +185,6 @@ __device__ __forceinline__ uint4 lds16(uint32_t addr)
 // Where byte `at` of a tile of D-byte rows lies (the copies' and descriptors' swizzle).
 template <int D> __device__ __forceinline__ uint32_t swizzled(uint32_t at) { return at ^ (((at >> 7) & (D == 128 ? 7u : 3u)) << 4); }
 
-// A worker's segments: consecutive tiles of one unit.
-struct Segment {
-    uint32_t req, rt, head, j, count, j0, nt;
-    Request r;
-};
-
 // GS: tokens that share a scale (64 where pages have at least as many, else 16).
 template <typename T, int D, int GS>
 __global__ void __launch_bounds__(640, 1)
@@ -200,7 +202,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
         for (uint32_t s = 0; s < F::kKS; s++) { mbar_init(&M.kfull[s], 1); mbar_init(&M.kfree[s], 1); }
         for (uint32_t s = 0; s < F::kVS; s++) { mbar_init(&M.vfull[s], 1); mbar_init(&M.vfree[s], 64); }
         for (uint32_t s = 0; s < F::kHS; s++) { mbar_init(&M.hfull[s], 64); mbar_init(&M.hfree[s], 1); }
-        for (uint32_t s = 0; s < 2; s++) { mbar_init(&M.sfull[s], 2); for (uint32_t q = 0; q < 4; q++) mbar_init(&M.pfull[s][q], 128); mbar_init(&M.ofull[s], 1); }
+        for (uint32_t s = 0; s < 2; s++) { mbar_init(&M.sfull[s], 2); mbar_init(&M.pfull[s][0], 256); mbar_init(&M.pfull[s][1], 256); mbar_init(&M.ofull[s], 1); }
         mbar_init(&M.qfull, 512);
         mbar_init(&M.fin, 1);
         M.dead = 0;
@@ -227,20 +229,22 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
     for (uint32_t i = tid; i < groups; i += 640)
         if (W.groups[i].base <= t_begin && (i + 1 == groups || t_begin < W.groups[i + 1].base)) M.first = i;
     __syncthreads();
-    // the segment that starts at tile t, group g being the one before or that of t
-    auto segment_at = [&](unsigned long long t, uint32_t& g) {
-        while (g + 1 < groups && W.groups[g + 1].base <= t) g++;
-        const Group G = W.groups[g];
-        Segment s;
-        s.req = G.req;
-        s.rt = G.rt;
-        s.r = request_of(a, G.req);
-        s.nt = group_tiles(a, s.r, G.rt, s.j0);
-        const unsigned long long off = t - G.base;
+    // s becomes the segment that starts at tile t; g: the group before, or that of t.  Inside a group only the head changes.
+    auto to_segment = [&](Segment& s, unsigned long long t, uint32_t& g) {
+        if (t == t_begin || t >= s.end) {
+            while (g + 1 < groups && W.groups[g + 1].base <= t) g++;
+            const Group G = W.groups[g];
+            s.req = G.req;
+            s.rt = G.rt;
+            s.r = request_of(a, G.req);
+            s.nt = group_tiles(a, s.r, G.rt, s.j0);
+            s.base = G.base;
+            s.end = G.base + (unsigned long long)s.nt * a.p.kv_heads;
+        }
+        const unsigned long long off = t - s.base;
         s.head = (uint32_t)(off / s.nt);
         s.j = (uint32_t)(off % s.nt);
         s.count = (uint32_t)min((unsigned long long)(s.nt - s.j), t_end - t);
-        return s;
     };
     if (t_begin < t_end) {
         uint32_t g = M.first;
@@ -252,8 +256,9 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
             // ---- copies: a lane per page
             uint32_t ks = 0, kp = 0, vs = 0, vp = 0, ring = 0;
             const bool copy = !(a.inject & kInjectNoCopy);
+            Segment s = {};
             while (t < t_end) {
-                const Segment s = segment_at(t, g);
+                to_segment(s, t, g);
                 const int32_t* row = a.table + (size_t)s.req * a.table_stride;
                 for (uint32_t c = 0; c < s.count; c++) {
                     const uint32_t first = (s.j0 + s.j + c) * 128u;
@@ -313,8 +318,9 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                 mma_commit(bar(M.sfull[w]), leader);
                 if (leader) mbar_arrive_at(bar(M.sfull[w]));        // (and with it what came with the keys: the scales)
             };
+            Segment s = {};
             while (t < t_end) {
-                const Segment s = segment_at(t, g);
+                to_segment(s, t, g);
                 const uint32_t count = warp_uniform(s.count);
                 mbar_wait(bar(M.qfull), qp, a.wait_ns, &M.dead);
                 qp ^= 1u;
@@ -325,18 +331,18 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                 mma_commit(bar(M.kfree[ks]), leader);
                 if (++ks == F::kKS) { ks = 0; kp ^= 1u; }
                 for (uint32_t c = 0; c < count; c++) {
-                    mbar_wait(bar(M.hfull[hs]), hp, a.wait_ns, &M.dead);
+                    mbar_wait_hot(bar(M.hfull[hs]), hp, a.wait_ns, &M.dead);
                     const uint64_t v0 = smem_desc(base_s + F::oH + hs * F::kTile16, 16384, 1024, kSw128);
-                    if (c + 1 < count) mbar_wait(bar(M.kfull[ks]), kp, a.wait_ns, &M.dead);
+                    if (c + 1 < count) mbar_wait_hot(bar(M.kfull[ks]), kp, a.wait_ns, &M.dead);
 #pragma unroll
                     for (uint32_t w = 0; w < 2; w++) {
 #pragma unroll
-                        for (uint32_t q = 0; q < 4; q++) {              // the weights of 32 tokens: of both halves' first, then of their last
-                            mbar_wait(bar(M.pfull[w][q]), pp, a.wait_ns, &M.dead);
+                        for (uint32_t q = 0; q < 2; q++) {              // both halves' weights of their first 32 tokens, then of their last
+                            mbar_wait_hot(bar(M.pfull[w][q]), pp, a.wait_ns, &M.dead);
                             tmem_fence_after_sync();
 #pragma unroll
-                            for (uint32_t i = 0; i < 2; i++) {
-                                const uint32_t h = q % 2, kk = 4 * h + 2 * (q / 2) + i;
+                            for (uint32_t i = 0; i < 4; i++) {
+                                const uint32_t h = i / 2, kk = 4 * h + 2 * q + i % 2;
                                 mma_f16_ta(tmem + 256u + w * 128u, tmem + w * 128u + 64u * h + (kk % 4) * 8u, v0 + kk * 2048u / 16u,
                                            mma_desc(128, D, false, true), c + q + i > 0, leader);
                             }
@@ -365,8 +371,9 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
         } else {
             // ---- values to halves: thread = two tokens
             uint32_t vs = 0, vp = 0, hs = 0, hp = 0;
+            Segment s = {};
             while (t < t_end) {
-                const Segment s = segment_at(t, g);
+                to_segment(s, t, g);
                 const uint32_t row0 = s.rt * kManyRows, row1 = min(row0 + kManyRows, (uint32_t)s.r.rows * a.group) - 1u;
                 const Span sp = span_of(a, s.r.kv, s.r.kv - s.r.rows + (int32_t)(row0 / a.group), s.r.kv - s.r.rows + (int32_t)(row1 / a.group));
                 for (uint32_t c = 0; c < s.count; c++) {
@@ -426,7 +433,8 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                 return r != 0u;
             };
             while (t < t_end) {
-                Segment s = segment_at(t, g);
+                Segment s = M.seg[w];
+                to_segment(s, t, g);
                 bool live;
                 int32_t lo, hi, t0 = (int32_t)((s.j0 + s.j) * 128u + half * 64u);        // (of this thread's tokens)
                 {
@@ -441,9 +449,8 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                     // waits for its instructions, 20 cycles for each of them.)
                     constexpr uint32_t LPR = D / 8, RPI = 32 / LPR, BATCH = 4;          // lanes a row, rows a load
                     const uint32_t q0 = base_s + w * F::kQ, part = lane % LPR;
-#pragma unroll 1
-                    for (uint32_t r0 = 0; r0 < 16; r0 += RPI * BATCH) {
-                        uint4 q[BATCH];
+                    uint4 q[BATCH], ahead[BATCH];
+                    auto fetch = [&](uint32_t r0, uint4 (&q)[BATCH]) {
 #pragma unroll
                         for (uint32_t k = 0; k < BATCH; k++) {
                             const uint32_t gr = s.rt * kManyRows + (warp * 16u + r0 + k * RPI + lane / LPR);
@@ -452,6 +459,13 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                             if (gr < (uint32_t)s.r.rows * a.group)
                                 q[k] = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (size_t)qrow * a.q_row + (size_t)qh * a.q_head + part * 8u);
                         }
+                    };
+                    fetch(0, ahead);
+#pragma unroll 1
+                    for (uint32_t r0 = 0; r0 < 16; r0 += RPI * BATCH) {
+#pragma unroll
+                        for (uint32_t k = 0; k < BATCH; k++) q[k] = ahead[k];
+                        if (r0 + RPI * BATCH < 16) fetch(r0 + RPI * BATCH, ahead);
 #pragma unroll
                         for (uint32_t k = 0; k < BATCH; k++) {
                             const uint32_t row = warp * 16u + r0 + k * RPI + lane / LPR;       // (of the unit's 256)
@@ -495,6 +509,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                     async_proxy_fence();
                     mbar_arrive_at(bar(M.qfull));
                     both();
+                    if (half == 0u && line == 0u) M.seg[w] = s;       // (read again when the unit's part ends: in registers it would cost the loop)
                 }
                 const float f = M.f[local];
                 float m = -INFINITY, l = 0.0f, R = -INFINITY;       // R: what O refers to
@@ -503,7 +518,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                     auto written = [&](uint32_t part) {
                         tmem_wait_stores();
                         tmem_fence_before_sync();
-                        mbar_arrive_at(bar(M.pfull[w][2u * part + half]));
+                        mbar_arrive_at(bar(M.pfull[w][part]));
                     };
                     const bool whole = __all_sync(0xFFFFFFFFu, !live || (t0 >= lo && t0 + 64 <= hi));
                     mbar_wait(bar(M.sfull[w]), sp, a.wait_ns, &M.dead);
@@ -663,15 +678,15 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                             tmem_write16(tS + ch * 16u, pk);
                         }
                         written(0);
-                        mbar_arrive_at(bar(M.pfull[w][2u + half]));
+                        mbar_arrive_at(bar(M.pfull[w][1]));
                     }
                     sp ^= 1u;
                     ring = (ring + 1u) % F::kRing;
                 }
-                // the end of the unit's part (what it is about is asked for again: held through the loop it would cost registers there)
+                // the end of the unit's part
                 mbar_wait(bar(M.ofull[w]), sp ^ 1u, a.wait_ns, &M.dead);
                 tmem_fence_after_sync();
-                s = segment_at(t, g);
+                s = M.seg[w];
                 const uint32_t gr = s.rt * kManyRows + local, n_rows = (uint32_t)s.r.rows * a.group;
                 const uint32_t jq = gr / a.group, qrow = (uint32_t)s.r.start + jq, qh = s.head * a.group + gr % a.group;
                 const bool full = s.count == s.nt;
@@ -689,12 +704,11 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                 const bool nan = *(volatile uint32_t*)&M.nan_seen != 0u;
                 const int32_t row1 = (int32_t)min((s.rt + 1u) * kManyRows, n_rows) - 1;
                 const Span span = span_of(a, s.r.kv, s.r.kv - s.r.rows + (int32_t)(s.rt * kManyRows / a.group), s.r.kv - s.r.rows + row1 / (int32_t)a.group);
-                // a warp's rows go through its part of the queries' memory (their products are done), so that whole lines are stored: a row a thread,
-                // every store touched 32 lines
+                // Outputs: a warp's rows go through its part of the queries' memory (their products are done), so that whole lines are stored: a
+                // row a thread, every store touched 32 lines.  Parts have a layout for that: four channels of all rows side by side.
                 const uint32_t st0 = base_s + w * F::kQ + (warp % 8u) * 4096u;
-                unsigned char* dst0 = full ? reinterpret_cast<unsigned char*>(static_cast<T*>(a.out) + (size_t)qrow * a.o_row + (size_t)qh * a.o_head)
-                                           : reinterpret_cast<unsigned char*>(W.parts + (size_t)(blockIdx.x * 2u + slot) * kManyPartFloats + local * D);
-                if (!live) dst0 = nullptr;
+                T* const dst = live ? static_cast<T*>(a.out) + (size_t)qrow * a.o_row + (size_t)qh * a.o_head : nullptr;
+                float4* const part = reinterpret_cast<float4*>(W.parts + (size_t)(blockIdx.x * 2u + slot) * kManyPartFloats) + local;
 #pragma unroll 1
                 for (uint32_t ch = half * D / 64u; ch < (half + 1u) * D / 64u; ch++) {           // (either thread of a row has half of its channels)
                     float x[32];
@@ -716,8 +730,6 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                                 if ((v[i] & 0x7Fu) == 0x7Fu) x[i] = NAN;
                         }
                     }
-                    const uint32_t pieces = full ? 4 : 8;                // of 16 bytes, of a row
-                    const uint32_t mine = st0 + lane * 128u;
                     if (full) {
 #pragma unroll
                         for (uint32_t i = 0; i < 4; i++) {
@@ -725,22 +737,21 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
 #pragma unroll
                             for (uint32_t k = 0; k < 8; k++) from_float(o[k], x[8 * i + k]);
                             const uint4 v = *reinterpret_cast<const uint4*>(o);
-                            sts16(mine + ((i ^ (lane & 7u)) << 4), v.x, v.y, v.z, v.w);
+                            sts16(st0 + lane * 64u + ((i ^ ((lane >> 1) & 3u)) << 4), v.x, v.y, v.z, v.w);
                         }
+                        __syncwarp();
+#pragma unroll
+                        for (uint32_t k = 0; k < 4; k++) {
+                            const uint32_t r = k * 8u + lane / 4u, i = lane % 4u;
+                            T* to = reinterpret_cast<T*>(__shfl_sync(0xFFFFFFFFu, (unsigned long long)dst, r));
+                            const uint4 v = lds16(st0 + r * 64u + ((i ^ ((r >> 1) & 3u)) << 4));
+                            if (to) *reinterpret_cast<uint4*>(to + ch * 32u + i * 8u) = v;
+                        }
+                        __syncwarp();
                     } else {
 #pragma unroll
-                        for (uint32_t i = 0; i < 8; i++)
-                            sts16(mine + ((i ^ (lane & 7u)) << 4), __float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
+                        for (uint32_t i = 0; i < 8; i++) part[(ch * 8u + i) * kManyRows] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
                     }
-                    __syncwarp();
-#pragma unroll 4
-                    for (uint32_t r = lane / pieces; r < 32u; r += 32u / pieces) {
-                        const uint32_t i = lane % pieces;
-                        unsigned char* to = reinterpret_cast<unsigned char*>(__shfl_sync(0xFFFFFFFFu, (unsigned long long)dst0, r));
-                        const uint4 v = lds16(st0 + r * 128u + ((i ^ (r & 7u)) << 4));
-                        if (to) *reinterpret_cast<uint4*>(to + ch * pieces * 16u + i * 16u) = v;
-                    }
-                    __syncwarp();
                 }
                 tmem_fence_before_sync();
                 if (live && half == 0u) {
@@ -769,36 +780,42 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
     }
 }
 
-// The cut units' parts put together: block (worker, 8 rows).
+// The cut units' parts put together: block (worker, 8 rows), thread (four channels, row).
 template <typename T, int D>
-__global__ void __launch_bounds__(D)
+__global__ void __launch_bounds__(2 * D)
 k_attend_many_join(AttendArgs a)
 {
     grid_dep_wait();
     grid_dep_launch();
     const ManyWs W = many_ws(a.ws);
-    const uint32_t w0 = blockIdx.x, d = threadIdx.x;
+    const uint32_t w0 = blockIdx.x, i = blockIdx.y * 8u + threadIdx.x % 8u, d4 = threadIdx.x / 8u;
     const Cut cut = W.cuts[w0];
     if (!cut.valid) return;
     const Request r = request_of(a, cut.req);
-    for (uint32_t i = blockIdx.y * 8u; i < blockIdx.y * 8u + 8u; i++) {
-        const uint32_t gr = cut.rt * kManyRows + i;
-        if (gr >= (uint32_t)r.rows * a.group) return;
-        float m = -INFINITY, R = -INFINITY, l = 0.0f, o = 0.0f;
-        for (uint32_t w = w0; w <= cut.last; w++) {
-            const float* part = W.parts + (size_t)(w * 2u + (w == w0 ? cut.slot : 0u)) * kManyPartFloats;
-            const float4 s = *reinterpret_cast<const float4*>(part + kManyRows * 128 + 4 * i);
-            const float v = part[i * D + d];
-            const float m1 = fmaxf(m, s.x), R1 = fmaxf(R, s.y), mb = m1 == -INFINITY ? 0.0f : m1, rb = R1 == -INFINITY ? 0.0f : R1;
-            l = l * exp2_fast(m - mb) + s.z * exp2_fast(s.x - mb);
-            o = o * exp2_fast(R - rb) + v * exp2_fast(s.y - rb);
-            m = m1;
-            R = R1;
-        }
-        const uint32_t qrow = (uint32_t)r.start + gr / a.group, qh = cut.head * a.group + gr % a.group;
-        store_out<T>(a, qrow, qh, d, l == 0.0f ? 0.0f : o * exp2_fast(R == -INFINITY ? 0.0f : R - m) / l);
-        if (d == 0 && a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    const uint32_t gr = cut.rt * kManyRows + i;
+    if (gr >= (uint32_t)r.rows * a.group) return;
+    float m = -INFINITY, R = -INFINITY, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t w = w0; w <= cut.last; w++) {
+        const float* part = W.parts + (size_t)(w * 2u + (w == w0 ? cut.slot : 0u)) * kManyPartFloats;
+        const float4 s = *reinterpret_cast<const float4*>(part + kManyRows * 128 + 4 * i);
+        const float4 v = reinterpret_cast<const float4*>(part)[d4 * kManyRows + i];
+        const float m1 = fmaxf(m, s.x), R1 = fmaxf(R, s.y), mb = m1 == -INFINITY ? 0.0f : m1, rb = R1 == -INFINITY ? 0.0f : R1;
+        const float keep = exp2_fast(R - rb), take = exp2_fast(s.y - rb);
+        l = l * exp2_fast(m - mb) + s.z * exp2_fast(s.x - mb);
+        o[0] = o[0] * keep + v.x * take;
+        o[1] = o[1] * keep + v.y * take;
+        o[2] = o[2] * keep + v.z * take;
+        o[3] = o[3] * keep + v.w * take;
+        m = m1;
+        R = R1;
     }
+    const uint32_t qrow = (uint32_t)r.start + gr / a.group, qh = cut.head * a.group + gr % a.group;
+    const float factor = exp2_fast(R == -INFINITY ? 0.0f : R - m) / l;
+    __align__(8) T out[4];
+#pragma unroll
+    for (int k = 0; k < 4; k++) from_float(out[k], l == 0.0f ? 0.0f : o[k] * factor);
+    *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + (size_t)qrow * a.o_row + (size_t)qh * a.o_head + d4 * 4u) = *reinterpret_cast<const uint2*>(out);
+    if (d4 == 0 && a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
 }  // namespace wm
