@@ -504,10 +504,11 @@ wm_status wm_pages_plan(const int32_t* old_len, const int32_t* new_len, uint32_t
  *   ties to even; infinities become +-448, NaN stays NaN.
  * A power of two as scale costs at most one step of e4m3's range and nothing of its precision, and growing a
  * scale is exact for every code that stays normal.
- *   k, v    rows of kv_heads heads of the pool's head_dim, n_rows of them, of type WM_TYPE_*
+ *   k, v    rows of kv_heads heads of the pool's head_dim, n_rows (below 2^24) of them, of type WM_TYPE_*
  *   slots   [dev] i32[n_rows]
  *   report  [dev] or NULL: WM_ERR_ARG with the lowest row concerned where a slot is neither -1 nor in the pool, or
- *           is in its predecessor's page without being its successor; those rows are left out.
+ *           is in its predecessor's page without being its successor; those rows are left out, and those that
+ *           follow on them in that page.
  * No page may be written through two runs of rows of one call (two requests that append to the same page): its
  * contents are then unspecified, other pages are as they should be.
  */

@@ -1,5 +1,5 @@
 // The paged 8-bit cache: kernels (sm_100a) and C ABI.
-//   wm_pages_plan    : k_pages_plan
+//   wm_pages_plan    : k_pages_plan, and behind it k_pages_slots where there are many
 //   wm_pages_append  : k_pages_append
 //   wm_pages_attend  : k_attend_few -> k_attend_join; in front of them, where requests may have many rows, k_attend_groups ->
 //                      k_attend_many -> k_attend_many_join
@@ -42,12 +42,16 @@ static bool rows_ok(const wm_rows* r, uint32_t size)
     return r && r->ptr && aligned16(r->ptr) && (r->row_stride * size) % 16 == 0 && (r->head_stride * size) % 16 == 0;
 }
 
+constexpr uint64_t kAppendWarps = 148 * 64;
+// Rows a warp looks at: one while that many warps still fit the GPU a few times over, up to 32 beyond.
 template <typename T>
-static void append_launch(const AppendArgs& a, cudaStream_t s)
+static void append_launch(AppendArgs a, cudaStream_t s)
 {
-    const dim3 grid(a.n_rows, (2u * a.p.kv_heads + 7u) / 8u);
-    if (a.p.head_dim == 64) launch_after(k_pages_append<T, 64>, grid, 256, 0, s, a);
-    else launch_after(k_pages_append<T, 128>, grid, 256, 0, s, a);
+    const uint64_t units = 2ull * a.p.kv_heads;
+    a.per_warp = 1;
+    while (a.per_warp < 32u && units * ((a.n_rows + a.per_warp - 1u) / a.per_warp) > kAppendWarps) a.per_warp *= 2u;
+    const uint64_t jobs = units * ((a.n_rows + a.per_warp - 1u) / a.per_warp);
+    launch_after(a.p.head_dim == 64 ? k_pages_append<T, 64> : k_pages_append<T, 128>, (uint32_t)((jobs + 3u) / 4u), 128, 0, s, a);
 }
 
 // ---- what a device is asked once: its SMs, the kernels' shared memory
@@ -149,12 +153,16 @@ wm_status wm_pages_plan(const int32_t* old_len, const int32_t* new_len, uint32_t
     if (!shift || n_requests == 0 || n_requests > kMaxRequests || table_stride == 0 || n_slots >= (1u << 31)) return WM_ERR_ARG;
     if (n_pages == 0 || ((uint64_t)n_pages << shift) >= (1ull << 31) || (uint64_t)n_requests * table_stride >= (1ull << 31)) return WM_ERR_ARG;
     const PlanArgs a = {old_len, new_len, n_requests, page_tokens, shift, n_pages, table, table_stride, free_pages, free_count,
-                        free_count_out, start, slots, n_slots, report};
+                        free_count_out, start, slots, n_slots, n_slots > kPlanSlots, report};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const bool small = n_requests <= 1024u && n_slots <= 4096u;
+    const bool small = n_requests <= 1024u && n_slots <= kPlanSlots;
     launch_after_clustered(small ? k_pages_plan<false> : k_pages_plan<true>, small ? 1 : kPlanBlocks, kPlanThreads,
                            3u * (n_requests + 1u) * 4u, small ? 1 : kPlanBlocks, s, a);
-    g_launches = 1;
+    if (a.slots_apart) {
+        const uint32_t blocks = std::min((n_slots + 4u * kPlanThreads - 1u) / (4u * kPlanThreads), 1024u);
+        launch_after(k_pages_slots, blocks, kPlanThreads, (n_requests + 1u) * 4u, s, a);
+    }
+    g_launches = a.slots_apart ? 2 : 1;
     return launch_status();
 }
 
@@ -164,10 +172,10 @@ wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows
     uint32_t shift = 0;
     if (type < WM_TYPE_BF16 || type > WM_TYPE_F32) return WM_ERR_ARG;
     const uint32_t size = type == WM_TYPE_F32 ? 4 : 2;
-    if (!pages_ok(pages, shift) || !rows_ok(k, size) || !rows_ok(v, size) || !slots || n_rows >= (1u << 31)) return WM_ERR_ARG;
+    if (!pages_ok(pages, shift) || !rows_ok(k, size) || !rows_ok(v, size) || !slots || n_rows >= (1u << 24)) return WM_ERR_ARG;
     g_launches = 0;
     if (n_rows == 0) return WM_OK;
-    const AppendArgs a = {*pages, shift, {k->ptr, v->ptr}, {k->row_stride, v->row_stride}, {k->head_stride, v->head_stride}, slots, n_rows, report};
+    const AppendArgs a = {*pages, shift, {k->ptr, v->ptr}, {k->row_stride, v->row_stride}, {k->head_stride, v->head_stride}, slots, n_rows, 1, report};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (type == WM_TYPE_BF16) append_launch<__nv_bfloat16>(a, s);
     else if (type == WM_TYPE_F16) append_launch<__half>(a, s);

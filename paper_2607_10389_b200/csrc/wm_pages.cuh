@@ -37,12 +37,14 @@ struct PlanArgs {
     int32_t* start;
     int32_t* slots;
     uint32_t n_slots;
+    uint32_t slots_apart;       // the slots are k_pages_slots'
     wm_pages_report* rep;
 };
 
 constexpr uint32_t kPlanThreads = 1024;
 constexpr uint32_t kPlanPer = (kMaxRequests + kPlanThreads - 1) / kPlanThreads;    // requests a thread scans
 constexpr uint32_t kPlanBlocks = 8;                             // of a cluster
+constexpr uint32_t kPlanSlots = 4096;                           // slots up to which k_pages_plan lists them itself
 
 // The last i with s[i] <= x (s ascending, s[0] = 0, s[n] > x).
 __device__ __forceinline__ uint32_t last_not_above(const uint32_t* s, uint32_t n, uint32_t x)
@@ -149,6 +151,7 @@ k_pages_plan(PlanArgs a)
     }
     for (uint32_t i = gid; i <= a.n; i += step) a.start[i] = bad ? 0 : (int32_t)s_tok[i];
     if (bad) {
+        if (a.slots_apart) return;
         for (uint32_t t = gid; t < a.n_slots; t += step) a.slots[t] = -1;
         return;
     }
@@ -168,6 +171,7 @@ k_pages_plan(PlanArgs a)
         a.table[(size_t)i * a.stride + held + (k - s_take[i])] = taken(k);
     }
     for (uint32_t at = have + gid; at < after; at += step) a.free_pages[at] = given(at - have);
+    if (a.slots_apart) return;
     for (uint32_t t = gid; t < a.n_slots; t += step) {
         int32_t slot = -1;
         if (t < (uint32_t)total_tok) {
@@ -182,6 +186,44 @@ k_pages_plan(PlanArgs a)
     }
 }
 
+// Many slots, behind k_pages_plan: the table is complete, and the row offsets say which request a token is (a failed plan's
+// are all zero: every slot -1).  A thread has four tokens.  Measured: 1000 requests, 427,000 slots, pages of 16: 66 us with the slots in
+// k_pages_plan's eight blocks, PLAN_PROMPTS us this way.
+__global__ void __launch_bounds__(kPlanThreads)
+k_pages_slots(PlanArgs a)
+{
+    extern __shared__ uint32_t slots_smem[];            // [n + 1] the row offsets
+    grid_dep_wait();
+    grid_dep_launch();
+    for (uint32_t i = threadIdx.x; i <= a.n; i += kPlanThreads) slots_smem[i] = (uint32_t)a.start[i];
+    __syncthreads();
+    const uint32_t total = slots_smem[a.n];
+    for (uint32_t t0 = (blockIdx.x * kPlanThreads + threadIdx.x) * 4u; t0 < a.n_slots; t0 += gridDim.x * kPlanThreads * 4u) {
+        int32_t slot[4] = {-1, -1, -1, -1};
+        if (t0 < total) {
+            uint32_t i = last_not_above(slots_smem, a.n, t0), at_page = 0xFFFFFFFFu;
+            int32_t page = -1;
+#pragma unroll
+            for (uint32_t k = 0; k < 4; k++) {
+                const uint32_t t = t0 + k;
+                if (t >= total) break;
+                while (t >= slots_smem[i + 1]) { i++; at_page = 0xFFFFFFFFu; }
+                const uint32_t pos = (uint32_t)a.old_len[i] + (t - slots_smem[i]), at = pos >> a.page_shift;
+                if (at != at_page) { page = a.table[(size_t)i * a.stride + at]; at_page = at; }
+                if ((uint32_t)page < a.n_pages) slot[k] = (int32_t)(((uint32_t)page << a.page_shift) + (pos & (a.page - 1u)));
+                else pages_fault(a.rep, WM_ERR_ARG, i);
+            }
+        }
+        if (t0 + 4u <= a.n_slots && (reinterpret_cast<uintptr_t>(a.slots) & 15u) == 0) {
+            *reinterpret_cast<int4*>(a.slots + t0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+        } else {
+#pragma unroll
+            for (uint32_t k = 0; k < 4; k++)
+                if (t0 + k < a.n_slots) a.slots[t0 + k] = slot[k];
+        }
+    }
+}
+
 // ------------------------------------------------------------------ wm_pages_append
 
 struct AppendArgs {
@@ -190,7 +232,7 @@ struct AppendArgs {
     const void* src[2];             // keys, values
     uint64_t row_stride[2], head_stride[2];
     const int32_t* slots;
-    uint32_t n_rows;
+    uint32_t n_rows, per_warp;
     wm_pages_report* rep;
 };
 
@@ -259,75 +301,145 @@ __device__ __forceinline__ float power_not_below(float s)
     return __uint_as_float((e < 1u ? 1u : e > 254u ? 254u : e) << 23);
 }
 
-// A warp takes one run of rows that go into one page, for one head, keys or values: its largest value first, then the
-// codes of what the page keeps (only if the scale has grown), then the new rows'.
+// Eight elements a lane, LPR lanes a row.
+template <typename T> __device__ __forceinline__ void load8(const T* p, uint32_t (&w)[2 * sizeof(T)])
+{
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    if constexpr (sizeof(T) == 4) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p + 4);
+        w[4] = u.x; w[5] = u.y; w[6] = u.z; w[7] = u.w;
+    }
+}
+template <typename T> __device__ __forceinline__ void unpack8(const uint32_t (&w)[2 * sizeof(T)], float (&x)[8])
+{
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = __uint_as_float(w[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const float2 f = unpack2(w[i], T());
+            x[2 * i] = f.x; x[2 * i + 1] = f.y;
+        }
+    }
+}
+
+// A warp takes one run of rows that go into one page, for one head, keys or values: its largest value first, then the codes of
+// what the page keeps (only if the scale has grown), then the new rows'.  Bound by memory where runs are long (rows in once, codes
+// out once), by the chain slot, row, scale, code where they are short.  A warp looks at `a.per_warp` rows for the firsts of runs,
+// with a lane for each (one row a warp, prompts spent most of the call on starting warps that had nothing to do); a run of up to
+// kRows rows stays in registers between the two looks at it, of a longer one the last kRows do.
 template <typename T, int D>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(128)
 k_pages_append(AppendArgs a)
 {
-    constexpr int N = D / 32;
-    const uint32_t lane = threadIdx.x % 32, unit = blockIdx.y * 8u + threadIdx.x / 32, r0 = blockIdx.x;
+    constexpr uint32_t LPR = D / 8, RPL = 32 / LPR, KL = sizeof(T) == 4 ? 8 : 16, kRows = KL * RPL;      // lanes a row, rows a load, loads
+    const uint32_t lane = threadIdx.x % 32, part = lane % LPR, sub = lane / LPR;
+    const uint32_t units = 2u * a.p.kv_heads, job = blockIdx.x * 4u + threadIdx.x / 32, unit = job % units, row0 = job / units * a.per_warp;
     grid_dep_wait();
     grid_dep_launch();
-    if (unit >= 2u * a.p.kv_heads) return;
+    if (row0 >= a.n_rows) return;
     const uint32_t head = unit >> 1, side = unit & 1u;
     const uint32_t n_slots = a.p.n_pages << a.page_shift, mask = a.p.page_tokens - 1u;
-    const int32_t first = a.slots[r0];
-    if (first == -1) return;
-    if ((uint32_t)first >= n_slots) { if (unit == 0u && lane == 0) pages_fault(a.rep, WM_ERR_ARG, r0); return; }
-    const uint32_t page = (uint32_t)first >> a.page_shift;
-    if (r0 > 0) {
-        const int32_t before = a.slots[r0 - 1];
-        if (before >= 0 && (uint32_t)before < n_slots && (uint32_t)before >> a.page_shift == page) {
-            if (before + 1 != first && unit == 0u && lane == 0) pages_fault(a.rep, WM_ERR_ARG, r0);
-            return;                                     // not the first of its page, or out of order
+    bool leads = false;
+    if (lane < a.per_warp && row0 + lane < a.n_rows) {
+        const uint32_t r = row0 + lane;
+        const int32_t slot = a.slots[r], before = r > 0 ? a.slots[r - 1] : -1;
+        if (slot != -1) {
+            bool wrong = (uint32_t)slot >= n_slots;
+            if (!wrong) {
+                const bool same = (uint32_t)before < n_slots && (uint32_t)before >> a.page_shift == (uint32_t)slot >> a.page_shift;
+                wrong = same && before + 1 != slot;
+                leads = !same;
+            }
+            if (wrong && unit == 0u) pages_fault(a.rep, WM_ERR_ARG, r);
         }
     }
-    uint32_t run = 1;
-    const uint32_t off = (uint32_t)first & mask, most = min(a.p.page_tokens - off, a.n_rows - r0);
-    while (run < most && a.slots[r0 + run] == first + (int32_t)run) run++;
-
-    const T* src = static_cast<const T*>(a.src[side]) + (size_t)r0 * a.row_stride[side] + (size_t)head * a.head_stride[side] + lane * N;
-    float amax = 0.0f;
-    for (uint32_t r = 0; r < run; r++) {
-        float x[N];
-        load_row<T, N>(src + (size_t)r * a.row_stride[side], x);
+    for (uint32_t todo = __ballot_sync(0xFFFFFFFFu, leads); todo; todo &= todo - 1u) {
+        const uint32_t r0 = row0 + __ffs((int)todo) - 1u;
+        const uint32_t first = (uint32_t)a.slots[r0], page = first >> a.page_shift, off = first & mask;
+        const uint32_t most = min(a.p.page_tokens - off, a.n_rows - r0);
+        uint32_t run = 0;
+        for (;;) {                                       // how many rows follow one another
+            const bool next = run + lane < most && a.slots[r0 + run + lane] == (int32_t)(first + run + lane);
+            const uint32_t miss = __ballot_sync(0xFFFFFFFFu, !next);
+            run += miss ? __ffs((int)miss) - 1u : 32u;
+            if (miss) break;
+        }
+        float* scale_at = (side ? a.p.v_scale : a.p.k_scale) + (size_t)page * a.p.kv_heads + head;
+        const float old = off > 0 ? *scale_at : 0.0f;
+        const uint64_t stride = a.row_stride[side];
+        const T* src = static_cast<const T*>(a.src[side]) + (size_t)r0 * stride + (size_t)head * a.head_stride[side] + part * 8u;
+        uint32_t w[KL][2 * sizeof(T)], top = 0;
+        auto fetch = [&](uint32_t c0) {                  // rows c0 .. c0 + kRows - 1
 #pragma unroll
-        for (int i = 0; i < N; i++) amax = fabsf(x[i]) <= 3.402823466e38f ? fmaxf(amax, fabsf(x[i])) : amax;
-    }
-    amax = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax)));
-    float* scale_at = (side ? a.p.v_scale : a.p.k_scale) + (size_t)page * a.p.kv_heads + head;
-    unsigned char* codes = static_cast<unsigned char*>(side ? a.p.v : a.p.k) + (size_t)page * a.p.page_stride + (size_t)head * a.p.head_stride;
-    float scale = scale_for(amax);
-    if (off > 0) {
-        const float old = *scale_at;
-        scale = fmaxf(scale, power_not_below(old));
-        if (scale != old) {
-            const float ratio = __fdiv_rn(old, scale);
-            for (uint32_t t = 0; t < off; t++) {
-                unsigned char* c = codes + (size_t)t * a.p.token_stride + lane * N;
-                uint32_t in = N == 4 ? *reinterpret_cast<uint32_t*>(c) : *reinterpret_cast<uint16_t*>(c), out = 0;
+            for (uint32_t k = 0; k < KL; k++) {
+                const uint32_t r = c0 + k * RPL + sub;
+                if (r < run) {
+                    load8<T>(src + r * stride, w[k]);
+                } else {
 #pragma unroll
-                for (int i = 0; i < N; i += 2) {
-                    const uint32_t h = from_e4m3x2(in >> (8 * i));
-                    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-                    out |= to_e4m3x2(f.x * ratio, f.y * ratio) << (8 * i);
+                    for (uint32_t i = 0; i < 2 * sizeof(T); i++) w[k][i] = 0;
                 }
-                if (N == 4) *reinterpret_cast<uint32_t*>(c) = out; else *reinterpret_cast<uint16_t*>(c) = (uint16_t)out;
+            }
+        };
+        uint32_t c0 = 0;
+        for (;; c0 += kRows) {
+            fetch(c0);
+#pragma unroll
+            for (uint32_t k = 0; k < KL; k++) {
+                float x[8];
+                unpack8<T>(w[k], x);
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const uint32_t u = __float_as_uint(fabsf(x[i]));
+                    top = u < 0x7F800000u ? max(top, u) : top;
+                }
+            }
+            if (c0 + kRows >= run) break;
+        }
+        float scale = scale_for(__uint_as_float(__reduce_max_sync(0xFFFFFFFFu, top)));
+        unsigned char* codes = static_cast<unsigned char*>(side ? a.p.v : a.p.k) + (size_t)page * a.p.page_stride + (size_t)head * a.p.head_stride + part * 8u;
+        if (off > 0) {
+            scale = fmaxf(scale, power_not_below(old));
+            if (scale != old) {
+                const float ratio = __fdiv_rn(old, scale);
+#pragma unroll 4
+                for (uint32_t t = sub; t < off; t += RPL) {
+                    uint2* c = reinterpret_cast<uint2*>(codes + (size_t)t * a.p.token_stride);
+                    const uint2 in = *c;
+                    uint2 out;
+                    auto four = [&](uint32_t v) {
+                        const uint32_t h0 = from_e4m3x2(v), h1 = from_e4m3x2(v >> 16);
+                        const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+                        return to_e4m3x2(f0.x * ratio, f0.y * ratio) | to_e4m3x2(f1.x * ratio, f1.y * ratio) << 16;
+                    };
+                    out.x = four(in.x);
+                    out.y = four(in.y);
+                    *c = out;
+                }
             }
         }
-    }
-    __syncwarp();
-    if (lane == 0) *scale_at = scale;
-    const float inv = __fdiv_rn(1.0f, scale);           // a power of two: exact (2^-126 .. 2^127 have normal or subnormal inverses)
-    for (uint32_t r = 0; r < run; r++) {
-        float x[N];
-        load_row<T, N>(src + (size_t)r * a.row_stride[side], x);
-        uint32_t out = 0;
+        __syncwarp();
+        if (lane == 0) *scale_at = scale;
+        const float inv = __fdiv_rn(1.0f, scale);           // a power of two: exact (2^-126 .. 2^120 have inverses)
+        for (;;) {                                           // the rows at hand, then those before
 #pragma unroll
-        for (int i = 0; i < N; i += 2) out |= to_e4m3x2(x[i] * inv, x[i + 1] * inv) << (8 * i);
-        unsigned char* c = codes + (size_t)(off + r) * a.p.token_stride + lane * N;
-        if (N == 4) *reinterpret_cast<uint32_t*>(c) = out; else *reinterpret_cast<uint16_t*>(c) = (uint16_t)out;
+            for (uint32_t k = 0; k < KL; k++) {
+                const uint32_t r = c0 + k * RPL + sub;
+                if (r >= run) continue;
+                float x[8];
+                unpack8<T>(w[k], x);
+                uint2 out;
+                out.x = to_e4m3x2(x[0] * inv, x[1] * inv) | to_e4m3x2(x[2] * inv, x[3] * inv) << 16;
+                out.y = to_e4m3x2(x[4] * inv, x[5] * inv) | to_e4m3x2(x[6] * inv, x[7] * inv) << 16;
+                *reinterpret_cast<uint2*>(codes + (size_t)(off + r) * a.p.token_stride) = out;
+            }
+            if (c0 == 0) break;
+            c0 -= kRows;
+            fetch(c0);
+        }
     }
 }
 
