@@ -82,18 +82,22 @@ template <typename T, int D, int RT> struct Few {
     // three tiles of keys and values in flight, two where three would not leave room for a second block on the SM
     static constexpr uint32_t kRest = kNQ * D + 128 * kWP + 140 * RT + 2048;
     static constexpr uint32_t kStages = (3 * 32768 + kRest <= 115712 ? 3 : 2) * (128 / D);
-    static constexpr uint32_t kCols = kNQ + kNP <= 64 ? 64 : kNQ + kNP <= 128 ? 128 : 256;
+    // tensor memory: S, O of a tile, and for more than one group of eight rows the sums so far (l by token, o by channel)
+    static constexpr uint32_t cO = kNQ, cL = kNQ + kNP, cA = cL + (RT > 8 ? RT : 0), kUsed = cA + (RT > 8 ? RT : 0);
+    static constexpr uint32_t kCols = kUsed <= 64 ? 64 : kUsed <= 128 ? 128 : 256;
+    static_assert(kUsed <= 256, "two blocks share an SM's tensor memory");
     // shared memory, from a 1024-byte boundary on
     static constexpr uint32_t oQ = kStages * kStage, oP = oQ + (kNQ * D + 1023) / 1024 * 1024, oMisc = oP + 128 * kWP;
     struct Misc {
-        unsigned long long kfull[kStages], vfull[kStages], empty[kStages], sbar, obar, fin;
+        unsigned long long kfull[kStages], vfull[kStages], empty[kStages], sbar, obar, qbar, pbar, fin;
         float2 scales[kStages][8];        // (key scale, value scale) of the tile's pages
         float top[4][RT][2];              // a warp's largest score and largest weighted score
         alignas(16) float state[4][RT][4];            // per warp: m, R, factors of l and of o
-        float f[RT];                      // scale log2(e) / the query row's factor
+        alignas(16) float f[RT];          // scale log2(e) / the query row's factor
         float sum[4][RT];
         unsigned long long scan[4], total;
         unsigned long long first_prefix;
+        Request first;
         uint32_t first_req, tmem, dead, poison;
     };
     static constexpr uint32_t kSmem = oMisc + (uint32_t)sizeof(Misc) + 1024;
@@ -127,6 +131,33 @@ template <int RT> __device__ __forceinline__ UnitShape shape_of(const AttendArgs
     return u;
 }
 
+// Where byte `at` of a tile of D-byte rows lies (the copies' and descriptors' swizzle).
+template <int D> __device__ __forceinline__ uint32_t swizzled(uint32_t at) { return at ^ (((at >> 7) & (D == 128 ? 7u : 3u)) << 4); }
+
+// What the rows at positions pos0 (first) .. pos1 (last) see.
+struct Span {
+    int32_t any_lo, any_hi, all_lo, all_hi;
+};
+__device__ __forceinline__ int32_t sees_from(const AttendArgs& a, int32_t pos) { return a.window ? max(0, pos + 1 - (int32_t)min(a.window, 0x7FFFFFFFu)) : 0; }
+__device__ __forceinline__ int32_t sees_to(const AttendArgs& a, int32_t kv, int32_t pos) { return a.causal ? min(kv, max(0, pos + 1)) : kv; }
+__device__ __forceinline__ Span span_of(const AttendArgs& a, int32_t kv, int32_t pos0, int32_t pos1)
+{
+    return {sees_from(a, pos0), sees_to(a, kv, pos1), sees_from(a, pos1), sees_to(a, kv, pos0)};
+}
+
+// Four channels of a joined row: o in units of 2^R, l of 2^m.
+template <typename T>
+__device__ __forceinline__ void store_joined(const AttendArgs& a, const Request& r, uint32_t gr, uint32_t head, uint32_t d, float m, float R, float l, const float (&o)[4])
+{
+    const uint32_t qrow = (uint32_t)r.start + gr / a.group, qh = head * a.group + gr % a.group;
+    const float factor = exp2_fast(R == -INFINITY ? 0.0f : R - m);
+    __align__(8) T out[4];
+#pragma unroll
+    for (int k = 0; k < 4; k++) from_float(out[k], l == 0.0f ? 0.0f : o[k] * factor / l);
+    *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + (size_t)qrow * a.o_row + (size_t)qh * a.o_head + d) = *reinterpret_cast<const uint2*>(out);
+    if (d == 0 && a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+
 template <typename T> __device__ __forceinline__ void store_out(const AttendArgs& a, uint32_t row, uint32_t qh, uint32_t d, float v)
 {
     T r;
@@ -135,7 +166,7 @@ template <typename T> __device__ __forceinline__ void store_out(const AttendArgs
 }
 
 template <typename T, int D, int RT>
-__global__ void __launch_bounds__(160, 2)
+__global__ void __launch_bounds__(192, 2)
 k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap)
 {
     using F = Few<T, D, RT>;
@@ -150,6 +181,8 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
         for (uint32_t s = 0; s < F::kStages; s++) { mbar_init(&M.kfull[s], 1); mbar_init(&M.vfull[s], 1); mbar_init(&M.empty[s], 1); }
         mbar_init(&M.sbar, 1);
         mbar_init(&M.obar, 1);
+        mbar_init(&M.qbar, 128);
+        mbar_init(&M.pbar, 128);
         mbar_init(&M.fin, 1);
         M.dead = 0;
         M.poison = 0;
@@ -161,11 +194,12 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
     // this worker's share: each of 128 threads sums the tiles of some consecutive requests
     const uint32_t per = (a.n + 127u) / 128u;
     unsigned long long mine = 0, incl = 0;
+    Request mine_r = {};
     if (warp < 4) {
         for (uint32_t i = tid * per; i < min((tid + 1) * per, a.n); i++) {
-            const Request r = few_request_of(a, i);
-            if (!r.ok && blockIdx.x == 0) pages_fault(a.rep, WM_ERR_ARG, i);
-            if (r.rows) mine += shape_of<RT>(a, r).tiles;
+            mine_r = few_request_of(a, i);
+            if (!mine_r.ok && blockIdx.x == 0) pages_fault(a.rep, WM_ERR_ARG, i);
+            if (mine_r.rows) mine += shape_of<RT>(a, mine_r).tiles;
         }
         incl = mine;
 #pragma unroll
@@ -178,7 +212,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
     tmem_fence_before_sync();
     __syncthreads();
     tmem_fence_after_sync();
-    const uint32_t tmem = M.tmem, tS = tmem, tO = tmem + F::kNQ;
+    const uint32_t tmem = M.tmem;
     const unsigned long long total = M.scan[0] + M.scan[1] + M.scan[2] + M.scan[3];
     const unsigned long long workers = min((unsigned long long)gridDim.x, total);       // so that every share has a tile
     const unsigned long long t_begin = blockIdx.x < workers ? blockIdx.x * total / workers : total;
@@ -188,13 +222,15 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
         unsigned long long at = incl - mine;
         if (at <= t_begin && t_begin < incl) {
             uint32_t i = tid * per;
-            for (;; i++) {
-                const Request r = few_request_of(a, i);
-                const unsigned long long t = r.rows ? shape_of<RT>(a, r).tiles : 0;
-                if (t_begin < at + t) break;
-                at += t;
-            }
+            if (per > 1)
+                for (;; i++) {
+                    mine_r = few_request_of(a, i);
+                    const unsigned long long t = mine_r.rows ? shape_of<RT>(a, mine_r).tiles : 0;
+                    if (t_begin < at + t) break;
+                    at += t;
+                }
             M.first_req = i;
+            M.first = mine_r;
             M.first_prefix = at;
         }
     }
@@ -206,15 +242,23 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
 
     if (t_begin < t_end) {
         uint32_t req = M.first_req;
+        Request r = M.first;
+        UnitShape u = shape_of<RT>(a, r);
         unsigned long long prefix = M.first_prefix, t = t_begin;
+        auto to_request = [&]() {                        // r, u: of the request that has tile t
+            while (t >= prefix + u.tiles) {
+                prefix += u.tiles;
+                req++;
+                r = few_request_of(a, req);
+                u = r.rows ? shape_of<RT>(a, r) : UnitShape{0, 0, 1, 0};
+            }
+        };
         if (warp == 4) {
             // ---- the copies: a lane per page of the tile
             const uint32_t pages = 128u >> a.page_shift;
             uint32_t stage = 0, phase = 0;
             while (t < t_end) {
-                const Request r = few_request_of(a, req);
-                const UnitShape u = r.rows ? shape_of<RT>(a, r) : UnitShape{0, 0, 1, 0};
-                if (t >= prefix + u.tiles) { prefix += u.tiles; req++; continue; }
+                to_request();
                 const unsigned long long off = t - prefix;
                 const uint32_t unit = (uint32_t)(off / u.nt), j = (uint32_t)(off % u.nt), head = unit / u.row_tiles;
                 const uint32_t count = (uint32_t)min((unsigned long long)(u.nt - j), t_end - t);
@@ -262,33 +306,69 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                     while (!(mbar_try(bar(M.kfull[s]), parity) && mbar_try(bar(M.vfull[s]), parity)) && now_ns() - t0 < a.wait_ns) {}
                 }
             }
+        } else if (warp == 5) {
+            // ---- the products
+            uint32_t stage = 0, phase = 0, qphase = 0, pphase = 0;
+            const bool leader = elect_one();
+            auto scores = [&](uint32_t st) {
+                const uint64_t k0 = smem_desc(base_s + st * F::kStage, 16, 8 * D, F::kSwD), q0 = smem_desc(base_s + F::oQ, 16, 8 * D, F::kSwD);
+#pragma unroll
+                for (uint32_t kk = 0; kk < D / 32; kk++) mma_f8(tmem, k0 + kk * 2u, q0 + kk * 2u, mma_desc(128, F::kNQ, false, false), kk > 0, leader);
+                mma_commit(bar(M.sbar), leader);
+            };
+            while (t < t_end) {
+                to_request();
+                const unsigned long long off = t - prefix;
+                const uint32_t j = (uint32_t)(off % u.nt), count = warp_uniform((uint32_t)min((unsigned long long)(u.nt - j), t_end - t));
+                mbar_wait_hot(bar(M.kfull[stage]), phase, a.wait_ns, &M.dead);
+                mbar_wait_hot(bar(M.qbar), qphase, a.wait_ns, &M.dead);
+                qphase ^= 1u;
+                tmem_fence_after_sync();
+                scores(stage);
+                for (uint32_t c = 0; c < count; c++) {
+                    const uint32_t next = stage + 1 == F::kStages ? 0 : stage + 1, next_phase = next ? phase : phase ^ 1u;
+                    mbar_wait_hot(bar(M.vfull[stage]), phase, a.wait_ns, &M.dead);
+                    mbar_wait_hot(bar(M.pbar), pphase, a.wait_ns, &M.dead);
+                    pphase ^= 1u;
+                    tmem_fence_after_sync();
+                    const uint64_t v0 = smem_desc(base_s + stage * F::kStage + F::kHalf, 0, 8 * D, F::kSwD), p0 = smem_desc(base_s + F::oP, 0, 8 * F::kWP, F::kSwP);
+#pragma unroll
+                    for (uint32_t kk = 0; kk < 4; kk++)
+                        mma_f8(tmem + F::cO, v0 + kk * 2u * D, p0 + kk * 2u * F::kWP, mma_desc(128, F::kNP, true, true), kk > 0, leader);
+                    mma_commit(bar(M.obar), leader);
+                    mma_commit(bar(M.empty[stage]), leader);
+                    if (c + 1 < count) {
+                        mbar_wait_hot(bar(M.kfull[next]), next_phase, a.wait_ns, &M.dead);
+                        scores(next);
+                    }
+                    stage = next;
+                    phase = next_phase;
+                }
+                t += count;
+            }
+            if (*(volatile uint32_t*)&M.dead) {            // what was issued is done before the tensor memory is handed back
+                mma_commit(bar(M.fin), leader);
+                const uint32_t t0 = now_ns();
+                while (!mbar_try(bar(M.fin), 0) && now_ns() - t0 < a.wait_ns) {}
+            }
+            __syncwarp();
         } else {
-            // ---- scores, softmax, outputs: thread = token of the tile, then channel
+            // ---- scores, softmax, outputs: thread = token of the tile, then channel.  Rows in groups of eight, one after the other in the same
+            // code (unrolled over 32 rows it was so long that a block that runs it two or three times waited for its instructions: 26 us
+            // for three tiles)
+            constexpr uint32_t G8 = RT / 8;
             uint32_t stage = 0, kphase = 0, sphase = 0, ophase = 0;
             const uint32_t lane_t = tmem + ((warp * 32u) << 16);
             const uint32_t qs = base_s + F::oQ, ps = base_s + F::oP;
-            auto issue_scores = [&](uint32_t st) {
-                const uint32_t k0 = base_s + st * F::kStage;
-#pragma unroll
-                for (uint32_t kk = 0; kk < D / 32; kk++)
-                    mma_f8(tS, smem_desc(k0 + kk * 32u, 16, 8 * D, F::kSwD), smem_desc(qs + kk * 32u, 16, 8 * D, F::kSwD),
-                           mma_desc(128, F::kNQ, false, false), kk > 0);
-                mma_commit(bar(M.sbar));
-            };
             while (t < t_end) {
-                const Request r = few_request_of(a, req);
-                const UnitShape u = r.rows ? shape_of<RT>(a, r) : UnitShape{0, 0, 1, 0};
-                if (t >= prefix + u.tiles) { prefix += u.tiles; req++; continue; }
+                to_request();
                 const unsigned long long off = t - prefix;
                 const uint32_t unit = (uint32_t)(off / u.nt), j = (uint32_t)(off % u.nt), head = unit / u.row_tiles, rt = unit % u.row_tiles;
                 const uint32_t count = (uint32_t)min((unsigned long long)(u.nt - j), t_end - t);
                 const uint32_t row0 = rt * RT, rows = min((uint32_t)RT, (uint32_t)r.rows * a.group - row0);
                 // what the unit's first and last row see: [lo, hi)
                 const int32_t pos0 = r.kv - r.rows + (int32_t)(row0 / a.group), pos1 = r.kv - r.rows + (int32_t)((row0 + rows - 1u) / a.group);
-                const int32_t win = (int32_t)min(a.window, 0x7FFFFFFFu);
-                auto lo_of = [&](int32_t pos) { return win ? max(0, pos + 1 - win) : 0; };
-                auto hi_of = [&](int32_t pos) { return a.causal ? min(r.kv, max(0, pos + 1)) : r.kv; };
-                const int32_t any_lo = lo_of(pos0), any_hi = hi_of(pos1), all_lo = lo_of(pos1), all_hi = hi_of(pos0);
+                const Span sp = span_of(a, r.kv, pos0, pos1);
 
                 // the queries' pieces: TPR threads a row
                 {
@@ -337,67 +417,76 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                     }
                 }
                 async_proxy_fence();
-                asm volatile("bar.sync 1, 128;" ::: "memory");
-                if (tid == 0) {
-                    tmem_fence_after_sync();
-                    mbar_wait(bar(M.kfull[stage]), kphase, a.wait_ns, &M.dead);
-                    issue_scores(stage);
+                mbar_arrive_at(bar(M.qbar));
+                if (G8 > 1) {                             // the sums so far, in tensor memory
+                    const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 1
+                    for (uint32_t g = 0; g < 2 * G8; g++) tmem_write8(lane_t + F::cL + 8u * g, zero);
+                    tmem_wait_stores();
                 }
+                asm volatile("bar.sync 1, 128;" ::: "memory");
 
-                float o[RT], l[RT];
+                float o[8], l[8];                          // (of the one group, where there is one)
 #pragma unroll
-                for (uint32_t i = 0; i < RT; i++) { o[i] = 0.0f; l[i] = 0.0f; }
+                for (uint32_t i = 0; i < 8; i++) { o[i] = 0.0f; l[i] = 0.0f; }
                 float m_run = -INFINITY, r_run = -INFINITY;       // of row `lane`, the same in every warp
                 for (uint32_t c = 0; c < count; c++) {
                     const int32_t t0 = (int32_t)((u.j0 + j + c) * 128u), tok = t0 + (int32_t)tid;
+                    const bool whole = t0 >= sp.all_lo && t0 + 128 <= sp.all_hi;      // every row sees every token
                     mbar_wait(bar(M.sbar), sphase, a.wait_ns, &M.dead);
                     sphase ^= 1u;
                     tmem_fence_after_sync();
                     mbar_wait(bar(M.kfull[stage]), kphase, a.wait_ns, &M.dead);   // (long since done: for the scales behind it)
                     const float2 sc = M.scales[stage][tid >> a.page_shift];
-                    float x[RT];
-                    {
-                        float s[F::kNQ];
+                    const float lv = log2f(sc.y);
+                    auto scores_of = [&](uint32_t g, float (&x)[8]) {
+                        float s[F::kQP][8];
 #pragma unroll
-                        for (uint32_t i = 0; i < F::kNQ; i += 8) tmem_read8(lane_t + i, &s[i]);
+                        for (uint32_t p = 0; p < F::kQP; p++) tmem_read8(lane_t + p * RT + 8u * g, s[p]);
+                        float f[8];
+                        *reinterpret_cast<float4*>(f) = *reinterpret_cast<const float4*>(&M.f[8u * g]);
+                        *reinterpret_cast<float4*>(f + 4) = *reinterpret_cast<const float4*>(&M.f[8u * g + 4u]);
                         tmem_wait_loads();
 #pragma unroll
-                        for (uint32_t i = 0; i < RT; i++) {
-                            float v = s[RT + i];
-                            if (F::kQP == 3) v = fmaf(s[2 * RT + i], 0.0625f, v);
-                            x[i] = fmaf(v, 0.0625f, s[i]) * (M.f[i] * sc.x);
+                        for (uint32_t i = 0; i < 8; i++) {
+                            float v = s[1][i];
+                            if (F::kQP == 3) v = fmaf(s[F::kQP - 1][i], 0.0625f, v);
+                            x[i] = fmaf(v, 0.0625f, s[0][i]) * (f[i] * sc.x);
                         }
-                    }
-                    const bool whole = t0 >= all_lo && t0 + 128 <= all_hi;      // every row sees every token
-                    if (!whole) {
-                        uint32_t jq = row0 / a.group, g = row0 % a.group;
+                        if (!whole) {
+                            uint32_t jq = (row0 + 8u * g) / a.group, k = (row0 + 8u * g) % a.group;
 #pragma unroll
-                        for (uint32_t i = 0; i < RT; i++) {
-                            const int32_t pos = r.kv - r.rows + (int32_t)jq;
-                            if (!(tok >= lo_of(pos) && tok < hi_of(pos))) x[i] = -INFINITY;
-                            if (++g == a.group) { g = 0; jq++; }
+                            for (uint32_t i = 0; i < 8; i++) {
+                                const int32_t pos = r.kv - r.rows + (int32_t)jq;
+                                if (!(tok >= sees_from(a, pos) && tok < sees_to(a, r.kv, pos))) x[i] = -INFINITY;
+                                if (++k == a.group) { k = 0; jq++; }
+                            }
                         }
-                    }
-                    const float lv = log2f(sc.y);
+                    };
+                    float x[8];
                     {
                         float mt = -INFINITY, mr = -INFINITY;
+#pragma unroll 1
+                        for (uint32_t g = 0; g < G8; g++) {
+                            scores_of(g, x);
 #pragma unroll
-                        for (uint32_t i = 0; i < RT; i++) {
-                            const float v = warp_max(x[i]), w = warp_max(x[i] + lv);
-                            if (lane == i) { mt = v; mr = w; }
+                            for (uint32_t i = 0; i < 8; i++) {
+                                const float v = warp_max(x[i]), w = warp_max(x[i] + lv);
+                                if (lane == 8u * g + i) { mt = v; mr = w; }
+                            }
                         }
                         if (lane < RT) *reinterpret_cast<float2*>(M.top[warp][lane]) = make_float2(mt, mr);
                     }
                     asm volatile("bar.sync 1, 128;" ::: "memory");
                     if (lane < RT) {
-                        float mt = m_run, mr = r_run, mo = -INFINITY;
+                        float mt = m_run, mo = -INFINITY;
 #pragma unroll
                         for (uint32_t w = 0; w < 4; w++) {
                             const float2 v = *reinterpret_cast<const float2*>(M.top[w][lane]);
                             mt = fmaxf(mt, v.x);
                             mo = fmaxf(mo, v.y);
                         }
-                        mr = fmaxf(mr, mo);
+                        const float mr = fmaxf(r_run, mo);
                         const float mb = mt == -INFINITY ? 0.0f : mt, rb = mr == -INFINITY ? 0.0f : mr, ob = mo == -INFINITY ? 0.0f : mo;
                         // what exponents refer to, and the factors of l, of o and of this tile's outputs
                         *reinterpret_cast<float4*>(M.state[warp][lane]) = make_float4(mb, ob - 8.0f, exp2_fast(m_run - mb), exp2_fast(r_run - rb));
@@ -407,62 +496,59 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                     }
                     __syncwarp();
                     // weights: l in f32, pieces of p' 2^8 into P
-                    uint32_t piece[3][RT / 4];
-#pragma unroll
-                    for (uint32_t i = 0; i < RT; i += 2) {
-                        const float4 s0 = *reinterpret_cast<const float4*>(M.state[warp][i]), s1 = *reinterpret_cast<const float4*>(M.state[warp][i + 1]);
-                        l[i] = fmaf(l[i], s0.z, exp2_fast(x[i] - s0.x));
-                        l[i + 1] = fmaf(l[i + 1], s1.z, exp2_fast(x[i + 1] - s1.x));
-                        float y0 = exp2_fast(x[i] + lv - s0.y), y1 = exp2_fast(x[i + 1] + lv - s1.y);
-                        o[i] *= s0.w;
-                        o[i + 1] *= s1.w;
-#pragma unroll
-                        for (uint32_t p = 0; p < 3; p++) {
-                            const uint32_t cc = to_e4m3x2(y0, y1), h = from_e4m3x2(cc);
-                            const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
-                            y0 = (y0 - back.x) * 16.0f;
-                            y1 = (y1 - back.y) * 16.0f;
-                            if (i % 4 == 0) piece[p][i / 4] = cc; else piece[p][i / 4] |= cc << 16;
+#pragma unroll 1
+                    for (uint32_t g = 0; g < G8; g++) {
+                        if (G8 > 1) {
+                            tmem_read8(lane_t + F::cL + 8u * g, l);
+                            scores_of(g, x);
                         }
-                    }
-                    {
-                        uint32_t w[F::kWP / 4];
+                        uint32_t piece[3][2];
 #pragma unroll
-                        for (uint32_t i = 0; i < F::kWP / 4; i++) w[i] = 0;
+                        for (uint32_t i = 0; i < 8; i += 2) {
+                            const float4 s0 = *reinterpret_cast<const float4*>(M.state[warp][8u * g + i]), s1 = *reinterpret_cast<const float4*>(M.state[warp][8u * g + i + 1]);
+                            l[i] = fmaf(l[i], s0.z, exp2_fast(x[i] - s0.x));
+                            l[i + 1] = fmaf(l[i + 1], s1.z, exp2_fast(x[i + 1] - s1.x));
+                            float y0 = exp2_fast(x[i] + lv - s0.y), y1 = exp2_fast(x[i + 1] + lv - s1.y);
+                            if (G8 == 1) { o[i] *= s0.w; o[i + 1] *= s1.w; }
 #pragma unroll
-                        for (uint32_t p = 0; p < 3; p++)
-#pragma unroll
-                            for (uint32_t i = 0; i < RT / 4; i++) w[p * (RT / 4) + i] = piece[p][i];
+                            for (uint32_t p = 0; p < 3; p++) {
+                                const uint32_t cc = to_e4m3x2(y0, y1), h = from_e4m3x2(cc);
+                                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                                y0 = (y0 - back.x) * 16.0f;
+                                y1 = (y1 - back.y) * 16.0f;
+                                if (i % 4 == 0) piece[p][i / 4] = cc; else piece[p][i / 4] |= cc << 16;
+                            }
+                        }
+                        if (G8 > 1) tmem_write8(lane_t + F::cL + 8u * g, l);
                         const uint32_t swz = F::kWP == 128 ? tid & 7u : F::kWP == 64 ? (tid >> 1) & 3u : (tid >> 2) & 1u;
 #pragma unroll
-                        for (uint32_t ch = 0; ch < F::kNP / 16; ch++)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ps + tid * F::kWP + ((ch ^ swz) << 4)), "r"(w[4 * ch]),
-                                         "r"(w[4 * ch + 1]), "r"(w[4 * ch + 2]), "r"(w[4 * ch + 3]) : "memory");
+                        for (uint32_t p = 0; p < 3; p++) {
+                            const uint32_t byte = p * RT + 8u * g;
+                            asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(ps + tid * F::kWP + (((byte >> 4) ^ swz) << 4) + (byte & 8u)), "r"(piece[p][0]), "r"(piece[p][1]) : "memory");
+                        }
                     }
                     // values that not every row sees must not meet the others' zero weights as NaN: tokens that no row sees are cleared,
                     // NaN codes of tokens that some rows see are taken out and put into those rows' outputs below
                     uint32_t nan_at[D / 32];
                     if (!whole) {
                         mbar_wait(bar(M.vfull[stage]), kphase, a.wait_ns, &M.dead);
-                        const uint32_t v0 = base_s + stage * F::kStage + F::kHalf + tid * D;
-                        const bool any = tok >= any_lo && tok < any_hi, all = tok >= all_lo && tok < all_hi;
+                        const uint32_t v0 = base_s + stage * F::kStage + F::kHalf;
+                        const bool any = tok >= sp.any_lo && tok < sp.any_hi, all = tok >= sp.all_lo && tok < sp.all_hi;
 #pragma unroll
                         for (uint32_t i = 0; i < D / 32; i++) nan_at[i] = 0;
                         if (!any) {
 #pragma unroll
                             for (uint32_t i = 0; i < D; i += 16)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v0 + i), "r"(0u) : "memory");
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v0 + tid * D + i), "r"(0u) : "memory");
                         } else if (!all) {
                             uint32_t found = 0;
 #pragma unroll
                             for (uint32_t i = 0; i < D; i += 4) {
-                                // (the word's place among the channels: undo the swizzle)
-                                const uint32_t at = tid * D + i, word = (at ^ (((at >> 7) & (D == 128 ? 7u : 3u)) << 4)) - tid * D;
-                                const uint32_t v = lds_now<0>(v0 + word);
+                                const uint32_t at = v0 + swizzled<D>(tid * D + i), v = lds_now<0>(at);
                                 const uint32_t is = __vcmpeq4(v & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
                                 if (is) {
                                     found = 1;
-                                    sts_now(v0 + word, v & ~is);
+                                    sts_now(at, v & ~is);
                                     nan_at[i / 32] |= ((is & 1u) | (is >> 7 & 2u) | (is >> 14 & 4u) | (is >> 21 & 8u)) << (i % 32);
                                 }
                             }
@@ -470,67 +556,68 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                         }
                     }
                     async_proxy_fence();
+                    if (G8 > 1) tmem_wait_stores();
                     tmem_fence_before_sync();
-                    asm volatile("bar.sync 1, 128;" ::: "memory");
-                    const uint32_t next = stage + 1 == F::kStages ? 0 : stage + 1, next_phase = next ? kphase : kphase ^ 1u;
-                    const bool poison = *(volatile uint32_t*)&M.poison;
-                    if (tid == 0) {
-                        tmem_fence_after_sync();
-                        mbar_wait(bar(M.vfull[stage]), kphase, a.wait_ns, &M.dead);
-                        const uint32_t v0 = base_s + stage * F::kStage + F::kHalf;
-#pragma unroll
-                        for (uint32_t kk = 0; kk < 4; kk++)
-                            mma_f8(tO, smem_desc(v0 + kk * 32u * D, 0, 8 * D, F::kSwD), smem_desc(ps + kk * 32u * F::kWP, 0, 8 * F::kWP, F::kSwP),
-                                   mma_desc(128, F::kNP, true, true), kk > 0);
-                        mma_commit(bar(M.obar));
-                        mma_commit(bar(M.empty[stage]));
-                        if (c + 1 < count) {
-                            mbar_wait(bar(M.kfull[next]), next_phase, a.wait_ns, &M.dead);
-                            issue_scores(next);
-                        }
-                    }
+                    mbar_arrive_at(bar(M.pbar));
                     mbar_wait(bar(M.obar), ophase, a.wait_ns, &M.dead);
                     ophase ^= 1u;
                     tmem_fence_after_sync();
-                    {
-                        float s[F::kNP];
-#pragma unroll
-                        for (uint32_t i = 0; i < F::kNP; i += 8) tmem_read8(lane_t + F::kNQ + i, &s[i]);
-                        tmem_wait_loads();
-#pragma unroll
-                        for (uint32_t i = 0; i < RT; i++)
-                            o[i] = fmaf(fmaf(fmaf(s[2 * RT + i], 0.0625f, s[RT + i]), 0.0625f, s[i]), M.sum[warp][i], o[i]);
-                    }
+                    const bool poison = *(volatile uint32_t*)&M.poison != 0u;
                     if (poison) {                          // rare: the marks through P's memory (its MMAs are done)
 #pragma unroll
                         for (uint32_t i = 0; i < D / 32; i++) sts_now(ps + tid * 16u + 4u * i, whole ? 0u : nan_at[i]);
                         asm volatile("bar.sync 1, 128;" ::: "memory");
-                        const uint32_t d = tid % D;
-                        for (uint32_t k = 0; k < 128; k++) {
-                            if (!(lds_now<0>(ps + k * 16u + 4u * (d / 32u)) >> (d % 32u) & 1u)) continue;
-                            uint32_t jq = row0 / a.group, g = row0 % a.group;
+                    }
+#pragma unroll 1
+                    for (uint32_t g = 0; g < G8; g++) {
+                        float s[3][8];
 #pragma unroll
-                            for (uint32_t i = 0; i < RT; i++) {
-                                const int32_t pos = r.kv - r.rows + (int32_t)jq;
-                                if (t0 + (int32_t)k >= lo_of(pos) && t0 + (int32_t)k < hi_of(pos)) o[i] = NAN;
-                                if (++g == a.group) { g = 0; jq++; }
+                        for (uint32_t p = 0; p < 3; p++) tmem_read8(lane_t + F::cO + p * RT + 8u * g, s[p]);
+                        if (G8 > 1) tmem_read8(lane_t + F::cA + 8u * g, o);
+                        tmem_wait_loads();
+#pragma unroll
+                        for (uint32_t i = 0; i < 8; i++) {
+                            if (G8 > 1) o[i] *= M.state[warp][8u * g + i][3];
+                            o[i] = fmaf(fmaf(fmaf(s[2][i], 0.0625f, s[1][i]), 0.0625f, s[0][i]), M.sum[warp][8u * g + i], o[i]);
+                        }
+                        if (poison) {
+                            const uint32_t d = tid % D;
+#pragma unroll 1
+                            for (uint32_t k = 0; k < 128; k++) {
+                                if (!(lds_now<0>(ps + k * 16u + 4u * (d / 32u)) >> (d % 32u) & 1u)) continue;
+#pragma unroll
+                                for (uint32_t i = 0; i < 8; i++) {
+                                    const int32_t pos = r.kv - r.rows + (int32_t)((row0 + 8u * g + i) / a.group);
+                                    if (t0 + (int32_t)k >= sees_from(a, pos) && t0 + (int32_t)k < sees_to(a, r.kv, pos)) o[i] = NAN;
+                                }
                             }
                         }
+                        if (G8 > 1) tmem_write8(lane_t + F::cA + 8u * g, o);
+                    }
+                    if (G8 > 1) tmem_wait_stores();
+                    if (poison) {
+                        asm volatile("bar.sync 1, 128;" ::: "memory");
                         if (tid == 0) M.poison = 0;
                         asm volatile("bar.sync 1, 128;" ::: "memory");
                     }
-                    stage = next;
-                    kphase = next_phase;
+                    if (++stage == F::kStages) { stage = 0; kphase ^= 1u; }
                 }
 
                 // the end of the unit's part: l over the threads, then the outputs or the workspace
                 asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll 1
+                for (uint32_t g = 0; g < G8; g++) {
+                    if (G8 > 1) {
+                        tmem_read8(lane_t + F::cL + 8u * g, l);
+                        tmem_wait_loads();
+                    }
 #pragma unroll
-                for (uint32_t i = 0; i < RT; i++) {
-                    float v = l[i];
+                    for (uint32_t i = 0; i < 8; i++) {
+                        float v = l[i];
 #pragma unroll
-                    for (uint32_t d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-                    if (lane == i) M.sum[warp][i] = v;
+                        for (uint32_t d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+                        if (lane == i) M.sum[warp][8u * g + i] = v;
+                    }
                 }
                 if (lane < RT) *reinterpret_cast<float2*>(M.state[warp][lane]) = make_float2(m_run, r_run);
                 asm volatile("bar.sync 1, 128;" ::: "memory");
@@ -538,20 +625,28 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                 const bool full = count == u.nt;
                 const uint32_t slot = t == t_begin ? 0 : 1;
                 float* part = part_of(a.ws, blockIdx.x, slot);
+#pragma unroll 1
+                for (uint32_t g = 0; 8u * g < rows; g++) {
+                    if (G8 > 1) {
+                        tmem_read8(lane_t + F::cA + 8u * g, o);
+                        tmem_wait_loads();
+                    }
 #pragma unroll
-                for (uint32_t i = 0; i < RT; i++) {
-                    if (i >= rows) break;
-                    const float2 mr = *reinterpret_cast<const float2*>(M.state[warp][i]);
-                    float sum = (M.sum[0][i] + M.sum[1][i]) + (M.sum[2][i] + M.sum[3][i]);
-                    if (dead) sum = NAN;
-                    if (full) {
-                        const uint32_t gr = row0 + i, qrow = (uint32_t)r.start + gr / a.group, qh = head * a.group + gr % a.group;
-                        const float v = sum == 0.0f ? 0.0f : o[i] * exp2_fast(mr.y == -INFINITY ? 0.0f : mr.y - mr.x) / sum;
-                        if (tid < D) store_out<T>(a, qrow, qh, tid, v);
-                        if (tid == 0 && a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = sum == 0.0f ? -INFINITY : (mr.x + log2f(sum)) * 0.6931471805599453f;
-                    } else {
-                        if (tid < D) part[i * D + tid] = o[i];
-                        if (tid == 0) *reinterpret_cast<float4*>(part + kPartRows * 128 + 4 * i) = make_float4(mr.x, mr.y, sum, 0.0f);
+                    for (uint32_t k = 0; k < 8; k++) {
+                        const uint32_t i = 8u * g + k;
+                        if (i >= rows) break;
+                        const float2 mr = *reinterpret_cast<const float2*>(M.state[warp][i]);
+                        float sum = (M.sum[0][i] + M.sum[1][i]) + (M.sum[2][i] + M.sum[3][i]);
+                        if (dead) sum = NAN;
+                        if (full) {
+                            const uint32_t gr = row0 + i, qrow = (uint32_t)r.start + gr / a.group, qh = head * a.group + gr % a.group;
+                            const float v = sum == 0.0f ? 0.0f : o[k] * exp2_fast(mr.y == -INFINITY ? 0.0f : mr.y - mr.x) / sum;
+                            if (tid < D) store_out<T>(a, qrow, qh, tid, v);
+                            if (tid == 0 && a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = sum == 0.0f ? -INFINITY : (mr.x + log2f(sum)) * 0.6931471805599453f;
+                        } else {
+                            if (tid < D) part[i * D + tid] = o[k];
+                            if (tid == 0) *reinterpret_cast<float4*>(part + kPartRows * 128 + 4 * i) = make_float4(mr.x, mr.y, sum, 0.0f);
+                        }
                     }
                 }
                 if (!full && j == 0 && tid == 0) {
@@ -565,47 +660,44 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
             }
         }
     }
-    if (tid == 0 && *(volatile uint32_t*)&M.dead) {
-        pages_fault(a.rep, WM_ERR_TIMEOUT, 0);
-        mma_commit(bar(M.fin));                            // what was issued is done before the tensor memory is handed back
-        const uint32_t t0 = now_ns();
-        while (!mbar_try(bar(M.fin), 0) && now_ns() - t0 < a.wait_ns) {}
-    }
     tmem_fence_before_sync();
     __syncthreads();
+    if (tid == 0 && *(volatile uint32_t*)&M.dead) pages_fault(a.rep, WM_ERR_TIMEOUT, 0);
     if (warp == 4) {
         tmem_fence_after_sync();
         tmem_free<F::kCols>(tmem);
     }
 }
 
-// The cut units' parts put together: block (worker, row).
+// The cut units' parts put together: block (worker, eight rows), thread (row, four channels).
 template <typename T, int D, int RT>
-__global__ void __launch_bounds__(D)
+__global__ void __launch_bounds__(2 * D)
 k_attend_join(AttendArgs a)
 {
     grid_dep_wait();
     grid_dep_launch();
-    const uint32_t w0 = blockIdx.x, i = blockIdx.y, d = threadIdx.x;
+    const uint32_t w0 = blockIdx.x, i = blockIdx.y * 8u + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4u;
     const Cut cut = reinterpret_cast<const Cut*>(a.ws)[w0];
     if (!cut.valid) return;
     const Request r = request_of(a, cut.req);
     const uint32_t gr = cut.rt * RT + i;
     if (gr >= (uint32_t)r.rows * a.group) return;
-    float m = -INFINITY, R = -INFINITY, l = 0.0f, o = 0.0f;
+    float m = -INFINITY, R = -INFINITY, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
     for (uint32_t w = w0; w <= cut.last; w++) {
         const float* part = part_of(a.ws, w, w == w0 ? cut.slot : 0u);
-        const float4 s = *reinterpret_cast<const float4*>(part + kPartRows * 128 + 4 * i);
-        const float v = part[i * D + d];
+        const float4 s = *reinterpret_cast<const float4*>(part + kPartRows * 128 + 4 * i), v = *reinterpret_cast<const float4*>(part + i * D + d);
         const float m1 = fmaxf(m, s.x), R1 = fmaxf(R, s.y), mb = m1 == -INFINITY ? 0.0f : m1, rb = R1 == -INFINITY ? 0.0f : R1;
+        const float keep = exp2_fast(R - rb), take = exp2_fast(s.y - rb);
         l = l * exp2_fast(m - mb) + s.z * exp2_fast(s.x - mb);
-        o = o * exp2_fast(R - rb) + v * exp2_fast(s.y - rb);
+        o[0] = o[0] * keep + v.x * take;
+        o[1] = o[1] * keep + v.y * take;
+        o[2] = o[2] * keep + v.z * take;
+        o[3] = o[3] * keep + v.w * take;
         m = m1;
         R = R1;
     }
-    const uint32_t qrow = (uint32_t)r.start + gr / a.group, qh = cut.head * a.group + gr % a.group;
-    store_out<T>(a, qrow, qh, d, l == 0.0f ? 0.0f : o * exp2_fast(R == -INFINITY ? 0.0f : R - m) / l);
-    if (d == 0 && a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    store_joined<T>(a, r, gr, cut.head, d, m, R, l, o);
 }
 
 }  // namespace wm

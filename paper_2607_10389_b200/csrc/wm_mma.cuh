@@ -76,6 +76,11 @@ __device__ __forceinline__ void tmem_read32(uint32_t taddr, float* v)
                  "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
                  : WM_R8(w, 0), WM_R8(w, 8), WM_R8(w, 16), WM_R8(w, 24) : "r"(taddr) : "memory");
 }
+__device__ __forceinline__ void tmem_write8(uint32_t taddr, const float* v)
+{
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(v);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), WM_I8(w, 0) : "memory");
+}
 __device__ __forceinline__ void tmem_write16(uint32_t taddr, const uint32_t* w)
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"

@@ -114,8 +114,8 @@ static bool page_map(CUtensorMap* map, const wm_pages& p, void* codes)
 template <typename T, int D, int RT>
 static void few_launch(const AttendArgs& a, const CUtensorMap& k, const CUtensorMap& v, uint32_t workers, cudaStream_t s)
 {
-    launch_after(k_attend_few<T, D, RT>, workers, 160, Few<T, D, RT>::kSmem, s, a, k, v);
-    launch_after(k_attend_join<T, D, RT>, dim3(workers, RT), D, 0, s, a);
+    launch_after(k_attend_few<T, D, RT>, workers, 192, Few<T, D, RT>::kSmem, s, a, k, v);
+    launch_after(k_attend_join<T, D, RT>, dim3(workers, RT / 8), 2 * D, 0, s, a);
 }
 constexpr uint32_t kFewRows = 64;          // rows of a request and key head up to which the kernel for few rows has them
 template <typename T, int D>

@@ -74,16 +74,6 @@ __device__ __forceinline__ ManyWs many_ws(unsigned char* ws)
     return w;
 }
 
-// What the rows at positions pos0 (first) .. pos1 (last) see.
-struct Span {
-    int32_t any_lo, any_hi, all_lo, all_hi;
-};
-__device__ __forceinline__ int32_t sees_from(const AttendArgs& a, int32_t pos) { return a.window ? max(0, pos + 1 - (int32_t)min(a.window, 0x7FFFFFFFu)) : 0; }
-__device__ __forceinline__ int32_t sees_to(const AttendArgs& a, int32_t kv, int32_t pos) { return a.causal ? min(kv, max(0, pos + 1)) : kv; }
-__device__ __forceinline__ Span span_of(const AttendArgs& a, int32_t kv, int32_t pos0, int32_t pos1)
-{
-    return {sees_from(a, pos0), sees_to(a, kv, pos1), sees_from(a, pos1), sees_to(a, kv, pos0)};
-}
 __device__ __forceinline__ uint32_t group_tiles(const AttendArgs& a, const Request& r, uint32_t rt, uint32_t& j0)
 {
     const uint32_t row0 = rt * kManyRows, row1 = min(row0 + kManyRows, (uint32_t)r.rows * a.group) - 1u;
@@ -182,9 +172,6 @@ __device__ __forceinline__ uint4 lds16(uint32_t addr)
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
 }
-// Where byte `at` of a tile of D-byte rows lies (the copies' and descriptors' swizzle).
-template <int D> __device__ __forceinline__ uint32_t swizzled(uint32_t at) { return at ^ (((at >> 7) & (D == 128 ? 7u : 3u)) << 4); }
-
 // GS: tokens that share a scale (64 where pages have at least as many, else 16).
 template <typename T, int D, int GS>
 __global__ void __launch_bounds__(640, 1)
@@ -809,13 +796,7 @@ k_attend_many_join(AttendArgs a)
         m = m1;
         R = R1;
     }
-    const uint32_t qrow = (uint32_t)r.start + gr / a.group, qh = cut.head * a.group + gr % a.group;
-    const float factor = exp2_fast(R == -INFINITY ? 0.0f : R - m) / l;
-    __align__(8) T out[4];
-#pragma unroll
-    for (int k = 0; k < 4; k++) from_float(out[k], l == 0.0f ? 0.0f : o[k] * factor);
-    *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + (size_t)qrow * a.o_row + (size_t)qh * a.o_head + d4 * 4u) = *reinterpret_cast<const uint2*>(out);
-    if (d4 == 0 && a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    store_joined<T>(a, r, gr, cut.head, d4 * 4u, m, R, l, o);
 }
 
 }  // namespace wm
