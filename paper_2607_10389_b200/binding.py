@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -130,7 +131,6 @@ class Result:
 def read_result(result_dev: torch.Tensor) -> Result:
     """Copy a 40-byte device result record to the host (synchronises the current stream)."""
     raw = result_dev.cpu().numpy().tobytes()
-    import struct
     st, fb, nb, npres, wl, pb, cc, _ = struct.unpack("<iIIIQQII", raw)
     return Result(st, fb, nb, npres, wl, pb, cc)
 
@@ -411,10 +411,7 @@ class _CPages(ctypes.Structure):
                 ("head_dim", ctypes.c_uint32)]
 
 
-class _CRows(ctypes.Structure):
-    _fields_ = [("ptr", ctypes.c_void_p), ("row_stride", ctypes.c_uint64), ("head_stride", ctypes.c_uint64)]
-
-
+_pack_rows = struct.Struct("=QQQ").pack          # a wm_rows: pointer, strides of rows and heads
 TYPE_BF16, TYPE_F16, TYPE_F32 = 0, 1, 2
 _TYPES = {torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16, torch.float32: TYPE_F32}
 ATTEND_CAUSAL = 1
@@ -440,9 +437,17 @@ class Pages:
                 raise WmError(f"{what} must be a contiguous float32 tensor (n_pages, kv_heads) on the codes' device")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.kv_heads, self.page_tokens, self.head_dim = k.shape
-        self._c = _CPages(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
+        size = self.head_dim                     # (a stride along one page, head or token leads nowhere)
+        strides = [s if n > 1 else size for s, n in zip(k.stride(), k.shape)]
+        self._c = _CPages(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), strides[0], strides[1], strides[2],
                           self.n_pages, self.page_tokens, self.kv_heads, self.head_dim)
-        self._ref = ctypes.addressof(self._c)
+        self._ref, self._device = ctypes.addressof(self._c), k.get_device()
+
+    def handle(self, here: int) -> int:
+        """Address of the wm_pages record, for calls on device `here`."""
+        if self._device != here:
+            _refuse(self.k, "the pool", here)
+        return self._ref
 
 
 def new_pages(n_pages: int, page_tokens: int, kv_heads: int, head_dim: int, device="cuda") -> Pages:
@@ -474,29 +479,54 @@ def read_pages_report(report: torch.Tensor):
     return STATUS.get(status, str(status)), (first & 0xFFFFFFFF) - 1 if first else None
 
 
-def _i32(t: torch.Tensor, n, what: str) -> int:
+# The arguments' checks.  They are made on every call, so each is one pass of cheap questions; what is wrong is found out
+# only when something is.  `here`: the current device, on whose stream the kernels run.
+def _here() -> int:
+    if _device is None:
+        return torch.cuda.current_device()
+    try:
+        return _device()
+    except RuntimeError:                      # (no device at all)
+        return -2
+
+
+def _i32(t: torch.Tensor, n, what: str, here: int) -> int:
+    if t.dtype is torch.int32 and t.get_device() == here and t.is_contiguous() and (n is None or t.numel() == n):
+        return t.data_ptr()
+    _refuse(t, what, here)
+    raise WmError(f"{what} must be a contiguous int32 tensor" + (f" of {n} entries" if n is not None else ""))
+
+
+def _refuse(t: torch.Tensor, what: str, here: int) -> None:
     if not t.is_cuda:
         raise WmError(f"{what} must be a CUDA tensor (there is no CPU path)")
-    if t.dtype != torch.int32 or not t.is_contiguous() or (n is not None and t.numel() != n):
-        raise WmError(f"{what} must be a contiguous int32 tensor" + (f" of {n} entries" if n is not None else ""))
-    return t.data_ptr()
+    if t.get_device() != here:
+        raise WmError(f"{what} is on device {t.get_device()}, the current device is {here}")
 
 
-def _table(t: torch.Tensor, n_requests: int):
-    if not t.is_cuda or t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != n_requests or (t.numel() and t.stride(1) != 1) or \
-            t.stride(0) < t.shape[1]:
-        raise WmError(f"the table must be an int32 CUDA tensor of {n_requests} rows whose entries are contiguous")
-    if t.shape[0] > 1 and t.stride(0) != t.shape[1]:
-        raise WmError("the table must be contiguous")
-    return t.data_ptr(), t.shape[1]
+def _table(t: torch.Tensor, n_requests: int, here: int):
+    shape = t.shape
+    if t.dtype is torch.int32 and t.get_device() == here and len(shape) == 2 and shape[0] == n_requests and t.is_contiguous():
+        return t.data_ptr(), shape[1]
+    _refuse(t, "the table", here)
+    raise WmError(f"the table must be a contiguous int32 tensor of {n_requests} rows")
 
 
-def _rows(t: torch.Tensor, heads: int, dim: int, what: str) -> _CRows:
-    if not t.is_cuda:
-        raise WmError(f"{what} must be a CUDA tensor (there is no CPU path)")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.stride(2) != 1 or t.dtype not in _TYPES:
-        raise WmError(f"{what} must be (rows, {heads}, {dim}) in bfloat16, float16 or float32 with contiguous channels")
-    return _CRows(t.data_ptr(), t.stride(0), t.stride(1))
+def _rows(t: torch.Tensor, heads: int, dim: int, what: str, here: int) -> bytes:
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 3 and shape[1] == heads and shape[2] == dim and stride[2] == 1 and t.dtype in _TYPES and t.get_device() == here:
+        return _pack_rows(t.data_ptr(), stride[0] if shape[0] > 1 else 0, stride[1] if heads > 1 else 0)      # (no stride where it leads nowhere)
+    _refuse(t, what, here)
+    raise WmError(f"{what} must be (rows, {heads}, {dim}) in bfloat16, float16 or float32 with contiguous channels")
+
+
+def _report(report, here: int):
+    if report is None:
+        return None
+    if report.get_device() == here and report.numel() * report.element_size() >= PAGES_REPORT_BYTES and report.is_contiguous():
+        return report.data_ptr()
+    _refuse(report, "report", here)
+    raise WmError(f"report must be {PAGES_REPORT_BYTES} contiguous bytes")
 
 
 def wm_pages_plan(old_len: torch.Tensor, new_len: torch.Tensor, page_tokens: int, table: torch.Tensor, free_pages: torch.Tensor,
@@ -504,21 +534,27 @@ def wm_pages_plan(old_len: torch.Tensor, new_len: torch.Tensor, page_tokens: int
                   stream=None) -> None:
     """Block tables, free list, row offsets and slot map of a step (see include/wm.h).  All tensors are int32;
     `free_count_out` may be `free_count`."""
-    n = old_len.numel()
-    tab, width = _table(table, n)
-    _check(lib().wm_pages_plan(_i32(old_len, None, "old_len"), _i32(new_len, n, "new_len"), n, page_tokens, free_pages.numel(),
-                               tab, width, _i32(free_pages, None, "free_pages"), _i32(free_count, 1, "free_count"),
-                               _i32(free_count_out, 1, "free_count_out"), _i32(start, n + 1, "start"), _i32(slots, None, "slots"),
-                               slots.numel(), None if report is None else report.data_ptr(), _stream(stream)), "wm_pages_plan")
+    here, n = _here(), old_len.numel()
+    tab, width = _table(table, n, here)
+    n_slots = slots.numel()
+    rc = lib().wm_pages_plan(_i32(old_len, None, "old_len", here), _i32(new_len, n, "new_len", here), n, page_tokens, free_pages.numel(),
+                             tab, width, _i32(free_pages, None, "free_pages", here), _i32(free_count, 1, "free_count", here),
+                             _i32(free_count_out, 1, "free_count_out", here), _i32(start, n + 1, "start", here),
+                             _i32(slots, None, "slots", here) if n_slots else None, n_slots, _report(report, here), _stream(stream))
+    if rc:
+        _check(rc, "wm_pages_plan")
 
 
 def wm_pages_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, report=None, stream=None) -> None:
     """Rows of keys and values (rows, kv_heads, head_dim) into the slots of the pool (see include/wm.h)."""
-    ck, cv = (_rows(t, pages.kv_heads, pages.head_dim, what) for t, what in ((k, "k"), (v, "v")))
-    if k.dtype != v.dtype or k.shape[0] != v.shape[0]:
+    here, n = _here(), k.shape[0]
+    if k.dtype is not v.dtype or v.shape[0] != n:
         raise WmError("k and v must have the same type and number of rows")
-    _check(lib().wm_pages_append(pages._ref, ctypes.byref(ck), ctypes.byref(cv), _TYPES[k.dtype], _i32(slots, k.shape[0], "slots"),
-                                 k.shape[0], None if report is None else report.data_ptr(), _stream(stream)), "wm_pages_append")
+    rc = lib().wm_pages_append(pages.handle(here), _rows(k, pages.kv_heads, pages.head_dim, "k", here),
+                               _rows(v, pages.kv_heads, pages.head_dim, "v", here), _TYPES[k.dtype], _i32(slots, n, "slots", here), n,
+                               _report(report, here), _stream(stream))
+    if rc:
+        _check(rc, "wm_pages_append")
 
 
 def wm_pages_attend(pages: Pages, table: torch.Tensor, kv_len: torch.Tensor, q_start: torch.Tensor, q: torch.Tensor,
@@ -526,16 +562,21 @@ def wm_pages_attend(pages: Pages, table: torch.Tensor, kv_len: torch.Tensor, q_s
                     max_q=None, report=None, stream=None) -> None:
     """Attention of the rows q (rows, q_heads, head_dim) over the pool into `out` (see include/wm.h).  `scale` is
     head_dim ** -0.5 unless given; `max_q` the most rows a request has (all of q's unless given)."""
-    n, rows, heads = kv_len.numel(), q.shape[0], q.shape[1] if q.dim() == 3 else 0
-    cq, co = (_rows(t, heads, pages.head_dim, what) for t, what in ((q, "q"), (out, "out")))
-    if out.dtype != q.dtype or out.shape != q.shape:
-        raise WmError("out must have q's type and shape")
-    if lse is not None and (not lse.is_cuda or lse.dtype != torch.float32 or lse.shape != (rows, heads) or not lse.is_contiguous()):
-        raise WmError(f"lse must be a contiguous float32 CUDA tensor ({rows}, {heads})")
-    tab, width = _table(table, n)
-    _check(lib().wm_pages_attend(pages._ref, tab, width, _i32(kv_len, None, "kv_len"), _i32(q_start, n + 1, "q_start"), n,
-                                 ctypes.byref(cq), ctypes.byref(co), _TYPES[q.dtype], None if lse is None else lse.data_ptr(), rows,
-                                 heads, rows if max_q is None else int(max_q),
-                                 pages.head_dim ** -0.5 if scale is None else float(scale), ATTEND_CAUSAL if causal else 0,
-                                 int(window), workspace.data_ptr(), workspace.numel(),
-                                 None if report is None else report.data_ptr(), _stream(stream)), "wm_pages_attend")
+    here, n, shape, dim = _here(), kv_len.numel(), q.shape, pages.head_dim
+    if len(shape) != 3 or out.dtype is not q.dtype or out.shape != shape:
+        raise WmError("q must be (rows, heads, channels) and out have its type and shape")
+    rows, heads, _ = shape
+    if lse is not None and not (lse.dtype is torch.float32 and lse.get_device() == here and lse.shape == (rows, heads) and lse.is_contiguous()):
+        _refuse(lse, "lse", here)
+        raise WmError(f"lse must be a contiguous float32 tensor ({rows}, {heads})")
+    if workspace.get_device() != here or not workspace.is_contiguous():
+        _refuse(workspace, "workspace", here)
+        raise WmError("workspace must be contiguous")
+    tab, width = _table(table, n, here)
+    rc = lib().wm_pages_attend(pages.handle(here), tab, width, _i32(kv_len, None, "kv_len", here), _i32(q_start, n + 1, "q_start", here), n,
+                               _rows(q, heads, dim, "q", here), _rows(out, heads, dim, "out", here), _TYPES[q.dtype],
+                               None if lse is None else lse.data_ptr(), rows, heads, rows if max_q is None else max_q,
+                               dim ** -0.5 if scale is None else scale, ATTEND_CAUSAL if causal else 0, window, workspace.data_ptr(),
+                               workspace.numel() * workspace.element_size(), _report(report, here), _stream(stream))
+    if rc:
+        _check(rc, "wm_pages_attend")

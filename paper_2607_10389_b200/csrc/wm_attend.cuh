@@ -97,6 +97,7 @@ template <typename T, int D, int RT> struct Few {
         float sum[4][RT];
         unsigned long long scan[4], total;
         unsigned long long first_prefix;
+        int2 span[RT];                    // the tokens a row sees: from, to
         Request first;
         uint32_t first_req, tmem, dead, poison;
     };
@@ -119,6 +120,12 @@ struct UnitShape {
     uint32_t row_tiles, j0, nt;
     unsigned long long tiles;
 };
+// Worker w's first tile (the division in 32 bits where they hold it: the long one is a hundred instructions to wait for).
+__device__ __forceinline__ unsigned long long share_of(uint32_t w, unsigned long long total, unsigned long long workers)
+{
+    if (w >= workers) return total;
+    return total < (1u << 23) ? (unsigned long long)(w * (uint32_t)total / (uint32_t)workers) : w * total / workers;
+}
 template <int RT> __device__ __forceinline__ UnitShape shape_of(const AttendArgs& a, const Request& r)
 {
     UnitShape u;
@@ -215,8 +222,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
     const uint32_t tmem = M.tmem;
     const unsigned long long total = M.scan[0] + M.scan[1] + M.scan[2] + M.scan[3];
     const unsigned long long workers = min((unsigned long long)gridDim.x, total);       // so that every share has a tile
-    const unsigned long long t_begin = blockIdx.x < workers ? blockIdx.x * total / workers : total;
-    const unsigned long long t_end = blockIdx.x < workers ? (blockIdx.x + 1ull) * total / workers : total;
+    const unsigned long long t_begin = share_of(blockIdx.x, total, workers), t_end = share_of(blockIdx.x + 1u, total, workers);
     if (warp < 4) {
         for (uint32_t w = 0; w < warp; w++) incl += M.scan[w];
         unsigned long long at = incl - mine;
@@ -259,8 +265,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
             uint32_t stage = 0, phase = 0;
             while (t < t_end) {
                 to_request();
-                const unsigned long long off = t - prefix;
-                const uint32_t unit = (uint32_t)(off / u.nt), j = (uint32_t)(off % u.nt), head = unit / u.row_tiles;
+                const uint32_t off = (uint32_t)(t - prefix), unit = off / u.nt, j = off - unit * u.nt, head = unit / u.row_tiles;
                 const uint32_t count = (uint32_t)min((unsigned long long)(u.nt - j), t_end - t);
                 const int32_t* row = a.table + (size_t)req * a.table_stride;
                 for (uint32_t c = 0; c < count; c++) {
@@ -318,8 +323,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
             };
             while (t < t_end) {
                 to_request();
-                const unsigned long long off = t - prefix;
-                const uint32_t j = (uint32_t)(off % u.nt), count = warp_uniform((uint32_t)min((unsigned long long)(u.nt - j), t_end - t));
+                const uint32_t j = (uint32_t)(t - prefix) % u.nt, count = warp_uniform((uint32_t)min((unsigned long long)(u.nt - j), t_end - t));
                 mbar_wait_hot(bar(M.kfull[stage]), phase, a.wait_ns, &M.dead);
                 mbar_wait_hot(bar(M.qbar), qphase, a.wait_ns, &M.dead);
                 qphase ^= 1u;
@@ -362,8 +366,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
             const uint32_t qs = base_s + F::oQ, ps = base_s + F::oP;
             while (t < t_end) {
                 to_request();
-                const unsigned long long off = t - prefix;
-                const uint32_t unit = (uint32_t)(off / u.nt), j = (uint32_t)(off % u.nt), head = unit / u.row_tiles, rt = unit % u.row_tiles;
+                const uint32_t off = (uint32_t)(t - prefix), unit = off / u.nt, j = off - unit * u.nt, head = unit / u.row_tiles, rt = unit % u.row_tiles;
                 const uint32_t count = (uint32_t)min((unsigned long long)(u.nt - j), t_end - t);
                 const uint32_t row0 = rt * RT, rows = min((uint32_t)RT, (uint32_t)r.rows * a.group - row0);
                 // what the unit's first and last row see: [lo, hi)
@@ -418,6 +421,10 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                 }
                 async_proxy_fence();
                 mbar_arrive_at(bar(M.qbar));
+                if (tid < RT) {
+                    const int32_t pos = r.kv - r.rows + (int32_t)((row0 + tid) / a.group);
+                    M.span[tid] = make_int2(sees_from(a, pos), sees_to(a, r.kv, pos));
+                }
                 if (G8 > 1) {                             // the sums so far, in tensor memory
                     const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll 1
@@ -439,6 +446,15 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                     mbar_wait(bar(M.kfull[stage]), kphase, a.wait_ns, &M.dead);   // (long since done: for the scales behind it)
                     const float2 sc = M.scales[stage][tid >> a.page_shift];
                     const float lv = log2f(sc.y);
+                    uint32_t seen = 0xFFFFFFFFu;          // by which rows
+                    if (!whole) {
+                        seen = 0;
+#pragma unroll 8
+                        for (uint32_t i = 0; i < RT; i++) {
+                            const int2 s = M.span[i];
+                            seen |= (tok >= s.x && tok < s.y ? 1u : 0u) << i;
+                        }
+                    }
                     auto scores_of = [&](uint32_t g, float (&x)[8]) {
                         float s[F::kQP][8];
 #pragma unroll
@@ -454,13 +470,9 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                             x[i] = fmaf(v, 0.0625f, s[0][i]) * (f[i] * sc.x);
                         }
                         if (!whole) {
-                            uint32_t jq = (row0 + 8u * g) / a.group, k = (row0 + 8u * g) % a.group;
 #pragma unroll
-                            for (uint32_t i = 0; i < 8; i++) {
-                                const int32_t pos = r.kv - r.rows + (int32_t)jq;
-                                if (!(tok >= sees_from(a, pos) && tok < sees_to(a, r.kv, pos))) x[i] = -INFINITY;
-                                if (++k == a.group) { k = 0; jq++; }
-                            }
+                            for (uint32_t i = 0; i < 8; i++)
+                                if (!(seen >> (8u * g + i) & 1u)) x[i] = -INFINITY;
                         }
                     };
                     float x[8];
@@ -587,8 +599,8 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                                 if (!(lds_now<0>(ps + k * 16u + 4u * (d / 32u)) >> (d % 32u) & 1u)) continue;
 #pragma unroll
                                 for (uint32_t i = 0; i < 8; i++) {
-                                    const int32_t pos = r.kv - r.rows + (int32_t)((row0 + 8u * g + i) / a.group);
-                                    if (t0 + (int32_t)k >= sees_from(a, pos) && t0 + (int32_t)k < sees_to(a, r.kv, pos)) o[i] = NAN;
+                                    const int2 s = M.span[8u * g + i];
+                                    if (t0 + (int32_t)k >= s.x && t0 + (int32_t)k < s.y) o[i] = NAN;
                                 }
                             }
                         }

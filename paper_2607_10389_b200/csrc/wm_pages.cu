@@ -51,7 +51,10 @@ static void append_launch(AppendArgs a, cudaStream_t s)
     a.per_warp = 1;
     while (a.per_warp < 32u && units * ((a.n_rows + a.per_warp - 1u) / a.per_warp) > kAppendWarps) a.per_warp *= 2u;
     const uint64_t jobs = units * ((a.n_rows + a.per_warp - 1u) / a.per_warp);
-    launch_after(a.p.head_dim == 64 ? k_pages_append<T, 64> : k_pages_append<T, 128>, (uint32_t)((jobs + 3u) / 4u), 128, 0, s, a);
+    constexpr int kMany = sizeof(T) == 4 ? 8 : 16, kFew = sizeof(T) == 4 ? 2 : 4;
+    const bool few = a.per_warp == 1u;
+    launch_after(a.p.head_dim == 64 ? (few ? k_pages_append<T, 64, kFew> : k_pages_append<T, 64, kMany>)
+                                    : (few ? k_pages_append<T, 128, kFew> : k_pages_append<T, 128, kMany>), (uint32_t)((jobs + 3u) / 4u), 128, 0, s, a);
 }
 
 // ---- what a device is asked once: its SMs, the kernels' shared memory

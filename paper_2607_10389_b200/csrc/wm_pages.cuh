@@ -330,11 +330,12 @@ template <typename T> __device__ __forceinline__ void unpack8(const uint32_t (&w
 // out once), by the chain slot, row, scale, code where they are short.  A warp looks at `a.per_warp` rows for the firsts of runs,
 // with a lane for each (one row a warp, prompts spent most of the call on starting warps that had nothing to do); a run of up to
 // kRows rows stays in registers between the two looks at it, of a longer one the last kRows do.
-template <typename T, int D>
+// KL: loads in registers; few where a warp looks at one row and most runs are short (so that all warps fit at once), else as many as pay.
+template <typename T, int D, int KL>
 __global__ void __launch_bounds__(128)
 k_pages_append(AppendArgs a)
 {
-    constexpr uint32_t LPR = D / 8, RPL = 32 / LPR, KL = sizeof(T) == 4 ? 8 : 16, kRows = KL * RPL;      // lanes a row, rows a load, loads
+    constexpr uint32_t LPR = D / 8, RPL = 32 / LPR, kRows = KL * RPL;      // lanes a row, rows a load
     const uint32_t lane = threadIdx.x % 32, part = lane % LPR, sub = lane / LPR;
     const uint32_t units = 2u * a.p.kv_heads, job = blockIdx.x * 4u + threadIdx.x / 32, unit = job % units, row0 = job / units * a.per_warp;
     grid_dep_wait();
@@ -342,10 +343,16 @@ k_pages_append(AppendArgs a)
     if (row0 >= a.n_rows) return;
     const uint32_t head = unit >> 1, side = unit & 1u;
     const uint32_t n_slots = a.p.n_pages << a.page_shift, mask = a.p.page_tokens - 1u;
+    // the next 32 slots, and the one before: runs that end among them need no further look
+    const uint32_t r = row0 + lane;
+    const int32_t slot = r < a.n_rows ? a.slots[r] : -1;
+    int32_t before = lane == 0 && r > 0 ? a.slots[r - 1] : -1;
+    {
+        const int32_t up = __shfl_up_sync(0xFFFFFFFFu, slot, 1);
+        if (lane > 0) before = up;
+    }
     bool leads = false;
-    if (lane < a.per_warp && row0 + lane < a.n_rows) {
-        const uint32_t r = row0 + lane;
-        const int32_t slot = a.slots[r], before = r > 0 ? a.slots[r - 1] : -1;
+    if (lane < a.per_warp && r < a.n_rows) {
         if (slot != -1) {
             bool wrong = (uint32_t)slot >= n_slots;
             if (!wrong) {
@@ -357,15 +364,16 @@ k_pages_append(AppendArgs a)
         }
     }
     for (uint32_t todo = __ballot_sync(0xFFFFFFFFu, leads); todo; todo &= todo - 1u) {
-        const uint32_t r0 = row0 + __ffs((int)todo) - 1u;
-        const uint32_t first = (uint32_t)a.slots[r0], page = first >> a.page_shift, off = first & mask;
+        const uint32_t at = __ffs((int)todo) - 1u, r0 = row0 + at;
+        const uint32_t first = (uint32_t)__shfl_sync(0xFFFFFFFFu, slot, at), page = first >> a.page_shift, off = first & mask;
         const uint32_t most = min(a.p.page_tokens - off, a.n_rows - r0);
-        uint32_t run = 0;
-        for (;;) {                                       // how many rows follow one another
+        // how many rows follow one another
+        uint32_t run = lane - at, miss = __ballot_sync(0xFFFFFFFFu, lane >= at && !(run < most && slot == (int32_t)(first + run)));
+        run = (miss ? __ffs((int)miss) - 1u : 32u) - at;
+        while (!miss) {
             const bool next = run + lane < most && a.slots[r0 + run + lane] == (int32_t)(first + run + lane);
-            const uint32_t miss = __ballot_sync(0xFFFFFFFFu, !next);
+            miss = __ballot_sync(0xFFFFFFFFu, !next);
             run += miss ? __ffs((int)miss) - 1u : 32u;
-            if (miss) break;
         }
         float* scale_at = (side ? a.p.v_scale : a.p.k_scale) + (size_t)page * a.p.kv_heads + head;
         const float old = off > 0 ? *scale_at : 0.0f;

@@ -206,8 +206,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
     const unsigned long long total = W.total[0];
     const uint32_t groups = (uint32_t)W.total[1];
     const unsigned long long workers = min((unsigned long long)gridDim.x, total);
-    const unsigned long long t_begin = blockIdx.x < workers ? blockIdx.x * total / workers : total;
-    const unsigned long long t_end = blockIdx.x < workers ? (blockIdx.x + 1ull) * total / workers : total;
+    const unsigned long long t_begin = share_of(blockIdx.x, total, workers), t_end = share_of(blockIdx.x + 1u, total, workers);
     if (tid == 0) {
         Cut none = {};
         W.cuts[blockIdx.x] = none;
@@ -228,9 +227,9 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
             s.base = G.base;
             s.end = G.base + (unsigned long long)s.nt * a.p.kv_heads;
         }
-        const unsigned long long off = t - s.base;
-        s.head = (uint32_t)(off / s.nt);
-        s.j = (uint32_t)(off % s.nt);
+        const uint32_t off = (uint32_t)(t - s.base);
+        s.head = off / s.nt;
+        s.j = off - s.head * s.nt;
         s.count = (uint32_t)min((unsigned long long)(s.nt - s.j), t_end - t);
     };
     if (t_begin < t_end) {

@@ -28,7 +28,7 @@ def _c_pages(**change):
 def _c_rows(**change):
     f = dict(ptr=1 << 20, row_stride=8 * 128, head_stride=128)
     f.update(change)
-    return wm._CRows(*[f[n] for n, _ in wm._CRows._fields_])
+    return wm._pack_rows(f["ptr"] or 0, f["row_stride"], f["head_stride"])
 
 
 BAD_PAGES = [dict(k=None), dict(v_scale=None), dict(k=8 + (1 << 20)), dict(page_stride=24), dict(token_stride=64), dict(token_stride=136),
@@ -40,8 +40,8 @@ BAD_PAGES = [dict(k=None), dict(v_scale=None), dict(k=8 + (1 << 20)), dict(page_
 def test_a_pool_that_breaks_the_rules_is_refused(change):
     lib, at = wm.lib(), 1 << 20
     p, r = _c_pages(**change), _c_rows()
-    assert lib.wm_pages_append(ctypes.addressof(p), ctypes.byref(r), ctypes.byref(r), 0, at, 1, None, None) == -1
-    assert lib.wm_pages_attend(ctypes.addressof(p), at, 4, at, at, 1, ctypes.byref(r), ctypes.byref(r), 0, None, 1, 8, 1, 1.0, 1, 0, at,
+    assert lib.wm_pages_append(ctypes.addressof(p), r, r, 0, at, 1, None, None) == -1
+    assert lib.wm_pages_attend(ctypes.addressof(p), at, 4, at, at, 1, r, r, 0, None, 1, 8, 1, 1.0, 1, 0, at,
                                1 << 30, None, None) == -1
 
 
@@ -50,13 +50,13 @@ def test_a_pool_that_breaks_the_rules_is_refused(change):
 def test_append_refuses_bad_arguments(change):
     at, p = 1 << 20, _c_pages()
     k, v = _c_rows(**change.get("k", {})), _c_rows(**change.get("v", {}))
-    assert wm.lib().wm_pages_append(ctypes.addressof(p), ctypes.byref(k), ctypes.byref(v), change.get("type", 0), change.get("slots", at),
+    assert wm.lib().wm_pages_append(ctypes.addressof(p), k, v, change.get("type", 0), change.get("slots", at),
                                     change.get("n_rows", 1), None, None) == -1
 
 
 def test_append_of_no_rows_launches_nothing():
     at, p, r = 1 << 20, _c_pages(), _c_rows()
-    assert wm.lib().wm_pages_append(ctypes.addressof(p), ctypes.byref(r), ctypes.byref(r), 0, at, 0, None, None) == 0
+    assert wm.lib().wm_pages_append(ctypes.addressof(p), r, r, 0, at, 0, None, None) == 0
     assert wm.last_launch_count() == 0
 
 
@@ -70,13 +70,13 @@ def test_attend_refuses_bad_arguments(change):
     q, o = _c_rows(**change.get("q", {})), _c_rows(**change.get("o", {}))
     g = lambda name, other: change.get(name, other)  # noqa: E731
     assert wm.lib().wm_pages_attend(ctypes.addressof(p), g("table", at), g("stride", 4), g("kv_len", at), g("q_start", at), g("n", 1),
-                                    ctypes.byref(q), ctypes.byref(o), g("type", 0), None, g("rows", 1), g("q_heads", 8), g("max_q", 1),
+                                    q, o, g("type", 0), None, g("rows", 1), g("q_heads", 8), g("max_q", 1),
                                     g("scale", 1.0), g("options", 1), g("window", 0), g("ws", at), g("ws_bytes", 1 << 30), None, None) == -1
 
 
 def test_attend_of_no_rows_launches_nothing_and_other_head_sizes_have_no_workspace():
     at, p, r = 1 << 20, _c_pages(), _c_rows()
-    assert wm.lib().wm_pages_attend(ctypes.addressof(p), at, 4, at, at, 1, ctypes.byref(r), ctypes.byref(r), 0, None, 0, 8, 1, 1.0, 1, 0,
+    assert wm.lib().wm_pages_attend(ctypes.addressof(p), at, 4, at, at, 1, r, r, 0, None, 0, 8, 1, 1.0, 1, 0,
                                     at, 1 << 30, None, None) == 0
     assert wm.last_launch_count() == 0
     assert wm.pages_workspace_bytes(96) == 0 and wm.pages_workspace_bytes(64) > 0
