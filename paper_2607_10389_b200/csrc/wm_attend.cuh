@@ -165,6 +165,32 @@ __device__ __forceinline__ void store_joined(const AttendArgs& a, const Request&
     if (d == 0 && a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
+// What a lane of the copying warp needs of a tile: its page (lane = page of the tile) and that page's scales.  They are asked for
+// ahead, the page two tiles and the scales one: one after the other in front of every copy they took longer than the tile.
+struct PageOf {
+    int32_t page;          // -1: none in this lane
+    bool bad;
+    float2 sc;
+};
+__device__ __forceinline__ uint32_t pages_in(const AttendArgs& a, uint32_t first, int32_t kv)
+{
+    const uint32_t tokens = first < (uint32_t)kv ? min(128u, (uint32_t)kv - first) : 0u;
+    return (tokens + a.p.page_tokens - 1u) >> a.page_shift;
+}
+__device__ __forceinline__ void ask_page(const AttendArgs& a, PageOf& p, const int32_t* row, uint32_t first, int32_t kv, uint32_t lane)
+{
+    p.page = lane < pages_in(a, first, kv) ? row[(first >> a.page_shift) + lane] : -1;
+    p.bad = lane < pages_in(a, first, kv) && (uint32_t)p.page >= a.p.n_pages;
+}
+__device__ __forceinline__ void ask_scales(const AttendArgs& a, PageOf& p, uint32_t head)
+{
+    p.sc = make_float2(p.bad ? NAN : 1.0f, p.bad ? 0.0f : 1.0f);       // NaN where a row sees a page that there is not; what it loads does not matter
+    if (p.page >= 0 && !p.bad) {
+        const size_t at = (size_t)p.page * a.p.kv_heads + head;
+        p.sc = make_float2(a.p.k_scale[at], a.p.v_scale[at]);
+    }
+}
+
 template <typename T> __device__ __forceinline__ void store_out(const AttendArgs& a, uint32_t row, uint32_t qh, uint32_t d, float v)
 {
     T r;
@@ -268,23 +294,20 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                 const uint32_t off = (uint32_t)(t - prefix), unit = off / u.nt, j = off - unit * u.nt, head = unit / u.row_tiles;
                 const uint32_t count = (uint32_t)min((unsigned long long)(u.nt - j), t_end - t);
                 const int32_t* row = a.table + (size_t)req * a.table_stride;
+                const uint32_t first0 = (u.j0 + j) * 128u;
+                PageOf now, next, later;
+                ask_page(a, now, row, first0, r.kv, lane);
+                ask_page(a, next, row, first0 + 128u, r.kv, lane);
+                ask_scales(a, now, head);
                 for (uint32_t c = 0; c < count; c++) {
-                    const uint32_t first = (u.j0 + j + c) * 128u;
-                    const uint32_t tokens = first < (uint32_t)r.kv ? min(128u, (uint32_t)r.kv - first) : 0u;
-                    const uint32_t n = (tokens + a.p.page_tokens - 1u) >> a.page_shift;       // pages with tokens
-                    int32_t page = 0;
-                    float2 sc = make_float2(0.0f, 0.0f);
-                    if (lane < n) {
-                        page = row[(first >> a.page_shift) + lane];
-                        if ((uint32_t)page < a.p.n_pages) {
-                            const size_t at = (size_t)page * a.p.kv_heads + head;
-                            sc = make_float2(a.p.k_scale[at], a.p.v_scale[at]);
-                        } else {
-                            sc = make_float2(NAN, 0.0f);       // NaN where a row sees it; what it loads does not matter
-                            page = 0;
-                            pages_fault(a.rep, WM_ERR_ARG, req);
-                        }
-                    }
+                    ask_page(a, later, row, first0 + (c + 2u) * 128u, r.kv, lane);
+                    ask_scales(a, next, head);
+                    const uint32_t n = pages_in(a, first0 + c * 128u, r.kv);
+                    const int32_t page = now.bad ? 0 : now.page;
+                    if (now.bad) pages_fault(a.rep, WM_ERR_ARG, req);
+                    const float2 sc = now.sc;
+                    now = next;
+                    next = later;
                     mbar_wait(bar(M.empty[stage]), phase ^ 1u, a.wait_ns, &M.dead);
                     if (lane < pages) M.scales[stage][lane] = sc;
                     __syncwarp();

@@ -246,23 +246,20 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
             while (t < t_end) {
                 to_segment(s, t, g);
                 const int32_t* row = a.table + (size_t)s.req * a.table_stride;
+                const uint32_t first0 = (s.j0 + s.j) * 128u;
+                PageOf now, next, later;
+                ask_page(a, now, row, first0, s.r.kv, lane);
+                ask_page(a, next, row, first0 + 128u, s.r.kv, lane);
+                ask_scales(a, now, s.head);
                 for (uint32_t c = 0; c < s.count; c++) {
-                    const uint32_t first = (s.j0 + s.j + c) * 128u;
-                    const uint32_t tokens = first < (uint32_t)s.r.kv ? min(128u, (uint32_t)s.r.kv - first) : 0u;
-                    const uint32_t n = (tokens + a.p.page_tokens - 1u) >> a.page_shift;
-                    int32_t page = 0;
-                    float2 sc = make_float2(1.0f, 0.0f);                 // (where no page is: any finite one)
-                    if (lane < n) {
-                        page = row[(first >> a.page_shift) + lane];
-                        if ((uint32_t)page < a.p.n_pages) {
-                            const size_t at = (size_t)page * a.p.kv_heads + s.head;
-                            sc = make_float2(a.p.k_scale[at], log2f(a.p.v_scale[at]));
-                        } else {
-                            sc = make_float2(NAN, 0.0f);
-                            page = 0;
-                            pages_fault(a.rep, WM_ERR_ARG, s.req);
-                        }
-                    }
+                    ask_page(a, later, row, first0 + (c + 2u) * 128u, s.r.kv, lane);
+                    ask_scales(a, next, s.head);
+                    const uint32_t n = pages_in(a, first0 + c * 128u, s.r.kv);
+                    const int32_t page = now.bad ? 0 : now.page;
+                    if (now.bad) pages_fault(a.rep, WM_ERR_ARG, s.req);
+                    float2 sc = make_float2(now.sc.x, now.bad ? 0.0f : log2f(now.sc.y));      // (1, 0) where no page is
+                    now = next;
+                    next = later;
                     const uint32_t bytes = (n << a.page_shift) * D;
                     mbar_wait(bar(M.kfree[ks]), kp ^ 1u, a.wait_ns, &M.dead);
                     const float least = warp_min(lane < n ? sc.y : INFINITY);
