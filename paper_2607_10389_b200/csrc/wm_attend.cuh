@@ -18,7 +18,7 @@ struct AttendArgs {
     uint32_t n_rows, q_heads, group;
     float scale;
     uint32_t causal, window;
-    uint32_t few_rows;          // requests with more rows (times heads that share a key head) are the other kernel's
+    uint32_t few_rows;          // requests with more rows (times heads that share a key head) are the kernel's for many
     unsigned char* ws;
     uint32_t wait_ns, inject;
     wm_pages_report* rep;

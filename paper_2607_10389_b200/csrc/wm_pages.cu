@@ -1,8 +1,8 @@
 // The paged 8-bit cache: kernels (sm_100a) and C ABI.
 //   wm_pages_plan    : k_pages_plan, and behind it k_pages_slots where there are many
 //   wm_pages_append  : k_pages_append
-//   wm_pages_attend  : k_attend_few -> k_attend_join; in front of them, where requests may have many rows, k_attend_groups ->
-//                      k_attend_many -> k_attend_many_join
+//   wm_pages_attend  : k_attend_few -> k_attend_join; in front of them, or in their place, where requests have many rows,
+//                      k_attend_groups -> k_attend_many -> k_attend_many_join
 #include <cstdint>
 #include <algorithm>
 #include <cmath>
@@ -120,19 +120,23 @@ static void few_launch(const AttendArgs& a, const CUtensorMap& k, const CUtensor
     launch_after(k_attend_few<T, D, RT>, workers, 192, Few<T, D, RT>::kSmem, s, a, k, v);
     launch_after(k_attend_join<T, D, RT>, dim3(workers, RT / 8), 2 * D, 0, s, a);
 }
-constexpr uint32_t kFewRows = 64;          // rows of a request and key head up to which the kernel for few rows has them
+// Rows of a request and key head up to which the kernel for few rows has them: what it can do in one pass over the cache.  Measured (us, the
+// kernel for few rows and the one for many; 8 key heads of 128): 16 requests of 8192 tokens 32 rows 94 and 134, 64 rows 164 and 136; 2
+// requests of 60000 tokens 91 and 125, 155 and 130; 2 of 1000 tokens 64 rows 20 and 30.
+constexpr uint32_t kFewRows = 32;
 template <typename T, int D>
-static void attend_launch(AttendArgs a, const CUtensorMap& k, const CUtensorMap& v, uint32_t sms, uint32_t rows, cudaStream_t s)
+static void attend_launch(AttendArgs a, const CUtensorMap& k, const CUtensorMap& v, uint32_t sms, uint32_t rows, bool alike, cudaStream_t s)
 {
     g_launches = 2;
     a.few_rows = 0xFFFFFFFFu;
     if (rows > kFewRows) {
-        a.few_rows = kFewRows;
+        a.few_rows = alike ? 0u : kFewRows;
         const uint32_t workers = std::min(sms, kMaxManyWorkers);
         launch_after(k_attend_groups, 1, 1024, 0, s, a);
         launch_after(a.p.page_tokens >= 64 ? k_attend_many<T, D, 64> : k_attend_many<T, D, 16>, workers, 640, Many<T, D>::kSmem, s, a, k, v);
-        launch_after(k_attend_many_join<T, D>, dim3(workers, kManyRows / 8), 2 * D, 0, s, a);
-        g_launches = 5;
+        launch_after(k_attend_many_join<T, D>, dim3(workers, kManyRows / 32), 2 * D, 0, s, a);
+        g_launches = alike ? 3 : 5;
+        if (alike) return;
     }
     const uint32_t workers = std::min(2u * sms, kMaxWorkers);
     if (rows <= 8) few_launch<T, D, 8>(a, k, v, workers, s);
@@ -216,12 +220,14 @@ wm_status wm_pages_attend(const wm_pages* pages, const int32_t* table, uint32_t 
     if (!page_map(&k, *pages, pages->k) || !page_map(&v, *pages, pages->v)) return WM_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const uint32_t rows = (uint32_t)std::min((uint64_t)std::min(max_q, n_rows) * a.group, (uint64_t)0xFFFFFFFFu);
+    // where there are rows enough for every request to have max_q of them, the kernel for many rows takes all there are (8 us less)
+    const bool alike = (uint64_t)n_requests * max_q <= n_rows;
     if (type == WM_TYPE_BF16) {
-        if (pages->head_dim == 64) attend_launch<__nv_bfloat16, 64>(a, k, v, dev->sms, rows, s);
-        else attend_launch<__nv_bfloat16, 128>(a, k, v, dev->sms, rows, s);
+        if (pages->head_dim == 64) attend_launch<__nv_bfloat16, 64>(a, k, v, dev->sms, rows, alike, s);
+        else attend_launch<__nv_bfloat16, 128>(a, k, v, dev->sms, rows, alike, s);
     } else {
-        if (pages->head_dim == 64) attend_launch<__half, 64>(a, k, v, dev->sms, rows, s);
-        else attend_launch<__half, 128>(a, k, v, dev->sms, rows, s);
+        if (pages->head_dim == 64) attend_launch<__half, 64>(a, k, v, dev->sms, rows, alike, s);
+        else attend_launch<__half, 128>(a, k, v, dev->sms, rows, alike, s);
     }
     return launch_status();
 }

@@ -103,9 +103,13 @@ k_attend_groups(AttendArgs a)
         __syncthreads();
         if (lane == 31) s_w[warp] = incl;
         __syncthreads();
-        unsigned long long before = 0;
-        all = 0;
-        for (uint32_t i = 0; i < 32; i++) { if (i < warp) before += s_w[i]; all += s_w[i]; }
+        all = s_w[lane];
+        unsigned long long before = lane < warp ? all : 0;
+#pragma unroll
+        for (uint32_t d = 16; d; d >>= 1) {
+            all += __shfl_xor_sync(0xFFFFFFFFu, all, d);
+            before += __shfl_xor_sync(0xFFFFFFFFu, before, d);
+        }
         return before + incl - v;
     };
     constexpr uint32_t kPer = (kMaxRequests + 1023u) / 1024u;
@@ -116,6 +120,7 @@ k_attend_groups(AttendArgs a)
         count[k] = 0;
         if (i < a.n) {
             const Request r = request_of(a, i);
+            if (!r.ok && a.few_rows == 0u) pages_fault(a.rep, WM_ERR_ARG, i);       // (else the kernel for few rows says so)
             const uint32_t rows = (uint32_t)r.rows * a.group;
             if ((uint32_t)r.rows > a.few_rows / a.group) count[k] = (rows + kManyRows - 1u) / kManyRows;
         }
@@ -763,7 +768,8 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
     }
 }
 
-// The cut units' parts put together: block (worker, 8 rows), thread (four channels, row).
+// The cut units' parts put together: block (worker, 32 rows), thread (four channels, four of the rows: their loads are on their way
+// together).
 template <typename T, int D>
 __global__ void __launch_bounds__(2 * D)
 k_attend_many_join(AttendArgs a)
@@ -771,28 +777,43 @@ k_attend_many_join(AttendArgs a)
     grid_dep_wait();
     grid_dep_launch();
     const ManyWs W = many_ws(a.ws);
-    const uint32_t w0 = blockIdx.x, i = blockIdx.y * 8u + threadIdx.x % 8u, d4 = threadIdx.x / 8u;
+    const uint32_t w0 = blockIdx.x, i0 = blockIdx.y * 32u + threadIdx.x % 8u, d4 = threadIdx.x / 8u;
     const Cut cut = W.cuts[w0];
     if (!cut.valid) return;
     const Request r = request_of(a, cut.req);
-    const uint32_t gr = cut.rt * kManyRows + i;
-    if (gr >= (uint32_t)r.rows * a.group) return;
-    float m = -INFINITY, R = -INFINITY, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t n_rows = (uint32_t)r.rows * a.group;
+    float m[4], R[4], l[4], o[4][4];
+#pragma unroll
+    for (uint32_t k = 0; k < 4; k++) {
+        m[k] = R[k] = -INFINITY;
+        l[k] = o[k][0] = o[k][1] = o[k][2] = o[k][3] = 0.0f;
+    }
     for (uint32_t w = w0; w <= cut.last; w++) {
         const float* part = W.parts + (size_t)(w * 2u + (w == w0 ? cut.slot : 0u)) * kManyPartFloats;
-        const float4 s = *reinterpret_cast<const float4*>(part + kManyRows * 128 + 4 * i);
-        const float4 v = reinterpret_cast<const float4*>(part)[d4 * kManyRows + i];
-        const float m1 = fmaxf(m, s.x), R1 = fmaxf(R, s.y), mb = m1 == -INFINITY ? 0.0f : m1, rb = R1 == -INFINITY ? 0.0f : R1;
-        const float keep = exp2_fast(R - rb), take = exp2_fast(s.y - rb);
-        l = l * exp2_fast(m - mb) + s.z * exp2_fast(s.x - mb);
-        o[0] = o[0] * keep + v.x * take;
-        o[1] = o[1] * keep + v.y * take;
-        o[2] = o[2] * keep + v.z * take;
-        o[3] = o[3] * keep + v.w * take;
-        m = m1;
-        R = R1;
+        float4 s[4], v[4];
+#pragma unroll
+        for (uint32_t k = 0; k < 4; k++) {                 // (rows that are not there were not written: read, and dropped below)
+            s[k] = *reinterpret_cast<const float4*>(part + kManyRows * 128 + 4 * (i0 + 8u * k));
+            v[k] = reinterpret_cast<const float4*>(part)[d4 * kManyRows + i0 + 8u * k];
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < 4; k++) {
+            const float m1 = fmaxf(m[k], s[k].x), R1 = fmaxf(R[k], s[k].y), mb = m1 == -INFINITY ? 0.0f : m1, rb = R1 == -INFINITY ? 0.0f : R1;
+            const float keep = exp2_fast(R[k] - rb), take = exp2_fast(s[k].y - rb);
+            l[k] = l[k] * exp2_fast(m[k] - mb) + s[k].z * exp2_fast(s[k].x - mb);
+            o[k][0] = o[k][0] * keep + v[k].x * take;
+            o[k][1] = o[k][1] * keep + v[k].y * take;
+            o[k][2] = o[k][2] * keep + v[k].z * take;
+            o[k][3] = o[k][3] * keep + v[k].w * take;
+            m[k] = m1;
+            R[k] = R1;
+        }
     }
-    store_joined<T>(a, r, gr, cut.head, d4 * 4u, m, R, l, o);
+#pragma unroll
+    for (uint32_t k = 0; k < 4; k++) {
+        const uint32_t gr = cut.rt * kManyRows + i0 + 8u * k;
+        if (gr < n_rows) store_joined<T>(a, r, gr, cut.head, d4 * 4u, m[k], R[k], l[k], o[k]);
+    }
 }
 
 }  // namespace wm
