@@ -433,7 +433,7 @@ typedef struct {
     void*    v;             /* [dev] the same for values, same strides */
     float*   k_scale;       /* [dev] f32[n_pages * kv_heads], finite and not negative */
     float*   v_scale;       /* [dev] */
-    uint64_t page_stride;   /* bytes; multiples of 16, the three in any order; no two elements share a byte */
+    uint64_t page_stride;   /* bytes; multiples of 16 below 2^40, the three in any order; no two elements share a byte */
     uint64_t head_stride;
     uint64_t token_stride;
     uint32_t n_pages;       /* 1 .. ; n_pages * page_tokens < 2^31 */
@@ -523,7 +523,8 @@ wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows
  *   out = sum_t softmax_t(scale * q . key_t) value_t,   lse = log sum_t exp(scale * q . key_t)
  * A row that sees nothing (a position below zero, no tokens) gets zeros and -infinity.  Rows behind the last request's are
  * left as they are.  Codes a row does not see do not touch it, whatever they hold (NaN included).
- *   table     [dev] i32[n_requests][table_stride], kv_len [dev] i32[n_requests], q_start [dev] i32[n_requests + 1]
+ *   table     [dev] i32[n_requests][table_stride], table_stride * page_tokens <= 2^30; kv_len [dev] i32[n_requests];
+ *             q_start [dev] i32[n_requests + 1]
  *   q, out    n_rows rows of q_heads heads of the pool's head_dim, WM_TYPE_BF16 or WM_TYPE_F16; must not overlap
  *   lse       [dev] f32[n_rows][q_heads] or NULL
  *   q_heads   a multiple of kv_heads, at most 64 * kv_heads; n_rows * q_heads / kv_heads <= 2^24

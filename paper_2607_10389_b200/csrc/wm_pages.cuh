@@ -188,7 +188,7 @@ k_pages_plan(PlanArgs a)
 
 // Many slots, behind k_pages_plan: the table is complete, and the row offsets say which request a token is (a failed plan's
 // are all zero: every slot -1).  A thread has four tokens.  Measured: 1000 requests, 427,000 slots, pages of 16: 66 us with the slots in
-// k_pages_plan's eight blocks, PLAN_PROMPTS us this way.
+// k_pages_plan's eight blocks, 11 us this way.
 __global__ void __launch_bounds__(kPlanThreads)
 k_pages_slots(PlanArgs a)
 {
@@ -327,7 +327,7 @@ template <typename T> __device__ __forceinline__ void unpack8(const uint32_t (&w
 
 // A warp takes one run of rows that go into one page, for one head, keys or values: its largest value first, then the codes of
 // what the page keeps (only if the scale has grown), then the new rows'.  Bound by memory where runs are long (rows in once, codes
-// out once), by the chain slot, row, scale, code where they are short.  A warp looks at `a.per_warp` rows for the firsts of runs,
+// out once: 103 MB of prompts in 24 us, 0.66 of the copy rate), by the chain slot, row, scale, code where they are short (3.5 us).  A warp looks at `a.per_warp` rows for the firsts of runs,
 // with a lane for each (one row a warp, prompts spent most of the call on starting warps that had nothing to do); a run of up to
 // kRows rows stays in registers between the two looks at it, of a longer one the last kRows do.
 // KL: loads in registers; few where a warp looks at one row and most runs are short (so that all warps fit at once), else as many as pay.

@@ -612,6 +612,80 @@ def test_attend_whose_waits_run_out_reports_it_gives_nan_and_the_next_call_is_ri
     _attend(pages, arrays, table, lens, rows, 4, torch.bfloat16, g, q=q)
 
 
+@gpu
+@pytest.mark.parametrize("rows", [[1, 1, 1], [3, 1, 2], [150, 130, 260]])
+def test_attend_over_keys_whose_scale_is_zero(rows):
+    g = torch.Generator().manual_seed(24)
+    lens = [300, 131, 260]
+    pages, arrays, table = _attend_case(lens, 16, 2, 64, g)
+    arrays[2][torch.rand(arrays[2].shape, generator=g) < 0.5] = 0.0
+    pages.k_scale.copy_(arrays[2])
+    _attend(pages, arrays, table, lens, rows, 4, torch.bfloat16, g)
+
+
+@gpu
+@pytest.mark.parametrize("rows", [[1, 1, 1], [3, 1, 2], [150, 130, 260]])
+def test_attend_over_values_that_are_all_zero(rows):
+    """As wm_pages_append stores zeros: codes of zero under the smallest scale, beside pages of ordinary ones."""
+    g = torch.Generator().manual_seed(25)
+    lens = [300, 131, 260]
+    pages, arrays, table = _attend_case(lens, 16, 2, 64, g)
+    for i in range(3):
+        for p in table[i][:ref.pages_of(lens[i], 16)][::3]:
+            arrays[1][p], arrays[3][p] = 0, 2.0 ** -126
+    pages.v.copy_(arrays[1]), pages.v_scale.copy_(arrays[3])
+    _attend(pages, arrays, table, lens, rows, 4, torch.bfloat16, g)
+    arrays[1].zero_(), arrays[3].fill_(2.0 ** -126)
+    pages.v.copy_(arrays[1]), pages.v_scale.copy_(arrays[3])
+    _attend(pages, arrays, table, lens, rows, 4, torch.bfloat16, g)
+
+
+@gpu
+@pytest.mark.parametrize("seed", range(24))
+def test_attend_of_mixed_batches(seed):
+    """Single tokens, drafts and prompts in one batch, any shape; told too few rows, the right number or none."""
+    r, g = random.Random(seed), torch.Generator().manual_seed(seed)
+    page, dim, kv_heads, group = r.choice([16, 32, 64, 128]), r.choice([64, 128]), r.choice([1, 2, 3]), r.choice([1, 2, 3, 5, 8, 16])
+    n = r.randint(1, 9)
+    lens = [r.choice([0, 1, 5, r.randint(1, 140), r.randint(100, 700)]) for _ in range(n)]
+    rows = [r.choice([0, 1, 1, 3, r.randint(0, 40), r.randint(0, 300)]) for _ in range(n)]
+    if not sum(rows):
+        rows[0] = 1
+    causal = r.random() < 0.7
+    window = r.choice([0, 0, 1, 17, 128, 333]) if causal else 0
+    pages, arrays, table = _attend_case(lens, page, kv_heads, dim, g, r.choice(["hnd", "nhd", "both"]))
+    _attend(pages, arrays, table, lens, rows, kv_heads * group, r.choice(DTYPES[:2]), g, causal, window, pad=r.choice([0, 4]),
+            max_q=r.choice([1, max(1, max(rows)), 5000]), strided=r.random() < 0.5)
+
+
+@gpu
+def test_calls_refuse_tensors_of_another_device(monkeypatch):
+    pages = wm.new_pages(4, 16, 1, 64)
+    i, table, x = _dev([1]), _dev([[0, 1]]), torch.zeros(1, 1, 64, device="cuda", dtype=torch.bfloat16)
+    ws = wm.new_pages_workspace(64)
+    monkeypatch.setattr(wm, "_device", lambda: 1)
+    with pytest.raises(wm.WmError, match="current device is 1"):
+        wm.wm_pages_plan(i, i, 16, table, _dev([2, 3]), i, i, _dev([0, 0]), _dev([0]))
+    with pytest.raises(wm.WmError, match="current device is 1"):
+        wm.wm_pages_append(pages, x, x, i)
+    with pytest.raises(wm.WmError, match="current device is 1"):
+        wm.wm_pages_attend(pages, table, i, _dev([0, 1]), x, x.clone(), ws)
+
+
+@gpu
+def test_many_slots_at_an_address_that_is_not_aligned():
+    n, page = 40, 16
+    r = random.Random(4)
+    old, new, width, table, free, count, n_slots = _plan_case(r, n, page, 300, 400, 0.1, 40 * n, 7)
+    assert n_slots > 4096
+    want = ref.plan(old, new, page, table, free, count, n_slots)
+    t, f, c = _dev(table), _dev(free), _dev([count])
+    start, slots = _dev([-9] * (n + 1)), _dev([-9] * (n_slots + 2))
+    wm.wm_pages_plan(_dev(old), _dev(new), page, t, f, c, c, start, slots[1:-1])
+    assert (t.tolist(), f.tolist(), int(c.item()), start.tolist()) == want[1:5]
+    assert slots.tolist() == [-9] + want[5] + [-9]
+
+
 # ---------------------------------------------------------------- together
 
 class Session:
@@ -732,6 +806,64 @@ def test_a_step_captured_into_a_graph_and_replayed():
         assert torch.equal(bufs[b][2], out) and torch.equal(bufs[b][3], lse)
     assert wm.read_pages_report(a.report) == ("OK", None) == wm.read_pages_report(b.report)
     assert torch.equal(a.pages.k, b.pages.k) and torch.equal(a.table, b.table) and torch.equal(a.count, b.count)
+
+
+@gpu
+def test_prompts_captured_into_a_graph_and_replayed_with_other_lengths():
+    g = torch.Generator().manual_seed(26)
+    most, page, dim = [400, 300, 200], 64, 128
+    pages, arrays, table = _attend_case(most, page, 2, dim, g)
+    tab, kv, start = _dev(table), _dev(most), _dev([0, 0, 0, 0])
+    q = torch.randn((500, 8, dim), generator=g).to(torch.bfloat16).cuda()
+    out, want, ws = torch.zeros_like(q), torch.zeros_like(q), wm.new_pages_workspace(dim)
+    call = lambda o: wm.wm_pages_attend(pages, tab, kv, start, q, o, ws, max_q=300)  # noqa: E731
+    call(out)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        with torch.cuda.graph(graph, stream=stream):
+            call(out)
+    for lens, starts in (([400, 300, 200], [0, 200, 300, 500]), ([400, 1, 128], [0, 300, 301, 301]), ([129, 300, 0], [0, 1, 260, 300]), ([400, 300, 200], [0, 0, 0, 0])):
+        kv.copy_(_dev(lens)), start.copy_(_dev(starts))
+        out.fill_(3.0), want.fill_(3.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        call(want)
+        assert torch.equal(out, want) and (out[starts[-1]:] == 3).all()
+
+
+_FIRST_IN_A_GRAPH = """
+import sys
+sys.path.insert(0, {root!r})
+import torch
+from paper_2607_10389_b200 import binding as wm
+p = wm.new_pages(4, 16, 1, 64)
+i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+old, new, table, free, count, start, slots = i32([0]), i32([3]), i32([[-1, -1]]), i32([3, 1, 2, 0]), i32([4]), i32([0, 0]), i32([0, 0, 0])
+x = torch.ones(3, 1, 64, device="cuda", dtype=torch.bfloat16)
+out, ws = torch.zeros_like(x), wm.new_pages_workspace(64)
+graph = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    wm.wm_pages_plan(old, new, 16, table, free, count, count, start, slots)
+    wm.wm_pages_append(p, x, x, slots)
+    wm.wm_pages_attend(p, table, new, start, x, out, ws, max_q=3)
+graph.replay()
+torch.cuda.synchronize()
+assert torch.equal(out, x) and slots.tolist() == [0, 1, 2] and count.item() == 3
+print("graph ok")
+"""
+
+
+@gpu
+def test_the_first_calls_of_a_process_may_be_captured():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, "-c", _FIRST_IN_A_GRAPH.format(root=root)], capture_output=True, text=True, timeout=600)
+    assert out.returncode == 0 and "graph ok" in out.stdout, out.stderr[-2000:]
 
 
 @gpu
