@@ -475,7 +475,7 @@ typedef struct {
  *     page * page_tokens + offset of position old_len[i] + j; slots behind the last token get -1.
  * Entries of the table that no request takes, and of the free list at or behind *free_count_out, are left as they are
  * (but those a request gives back and no request takes, which are written).  The call is made for replay in
- * a graph: free_count_out may be free_count.  It is the same for every input order of the free list.
+ * a graph: free_count_out may be free_count.
  *   old_len, new_len  [dev] i32[n_requests], 1 .. WM_PAGES_MAX_REQUESTS requests
  *   table      [dev] i32[n_requests][table_stride]: pages of each request in order; n_requests * table_stride < 2^31
  *   free_pages [dev] i32[n_pages]

@@ -78,8 +78,12 @@ template <typename T, int D> static bool few_ready_all() { return few_ready<T, D
 
 template <typename T, int D> static bool many_ready()
 {
-    for (const void* f : {(const void*)k_attend_many<T, D, 16>, (const void*)k_attend_many<T, D, 64>})
+    for (const void* f : {(const void*)k_attend_many<T, D, 16>, (const void*)k_attend_many<T, D, 64>}) {
+        // its warpgroups deal the registers that a block starts with out anew: with fewer than they count on they would wait for ever
+        cudaFuncAttributes attr;
+        if (cudaFuncGetAttributes(&attr, f) != cudaSuccess || attr.numRegs < (int)kManyRegs) return false;
         if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Many<T, D>::kSmem) != cudaSuccess) return false;
+    }
     return true;
 }
 

@@ -36,19 +36,22 @@ template <typename T, int D> struct Many {
     static constexpr uint32_t kQ = kQP * kTile8 > 32768 ? kQP * kTile8 : 32768;         // of 128 rows: the queries' pieces, then the outputs on their way
     static constexpr uint32_t oK = 2 * kQ, oV = oK + kKS * kTile8, oH = oV + kVS * kTile8, oMisc = oH + kHS * kTile16;
     struct Misc {
-        unsigned long long kfull[kKS], kfree[kKS], vfull[kVS], vfree[kVS], hfull[kHS], hfree[kHS], qfull, sfull[2], pfull[2][2], ofull[2], fin;
+        unsigned long long kfull[kKS], kfree[kKS], vfull[kVS], vfree[kVS], hfull[kHS], hfree[kHS], qfull, sfull[2], pfull[2][2], ofull[2], votes[2], fin;
         alignas(16) float2 scales[kRing][8];     // of every 16 tokens: (key scale, log2 of the value scale)
         float least[kRing];                     // the least of the logarithms
         float f[256];                           // of every row: |scale| log2(e) / its factor
         Segment seg[2];                         // what the two tiles' softmax threads are at
         float2 other[2][2][128];                // what the two halves of a row tell each other
-        uint32_t tmem, dead, nan_seen, first;
+        uint32_t tmem, dead, nan_seen, first, again[2][2];
     };
     static constexpr uint32_t kSmem = oMisc + (uint32_t)sizeof(Misc) + 1024;
 };
 
 // A weight of the reference's size is 2^kTop in f16; up to 2^kRoom more fits in (2^15 of 65504), and what is 2^-25 below is lost.
 constexpr float kTop = 1.0f, kRoom = 14.0f;
+// Registers a thread: at launch (five warpgroups), then of the four softmax warpgroups and of the fifth.
+constexpr uint32_t kManyRegs = 96, kSoftmaxRegs = 104, kOtherRegs = 64;
+static_assert(4 * kSoftmaxRegs + kOtherRegs <= 5 * kManyRegs, "dealt out from what there is at launch");
 constexpr uint32_t kManyRows = 256, kMaxManyWorkers = 160, kMaxGroups = 70000;
 // A tile of 256 rows of a request; its key heads' tiles stand one behind the other from `base` on.
 struct Group {
@@ -195,6 +198,9 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
         for (uint32_t s = 0; s < F::kVS; s++) { mbar_init(&M.vfull[s], 1); mbar_init(&M.vfree[s], 64); }
         for (uint32_t s = 0; s < F::kHS; s++) { mbar_init(&M.hfull[s], 64); mbar_init(&M.hfree[s], 1); }
         for (uint32_t s = 0; s < 2; s++) { mbar_init(&M.sfull[s], 2); mbar_init(&M.pfull[s][0], 256); mbar_init(&M.pfull[s][1], 256); mbar_init(&M.ofull[s], 1); }
+        mbar_init(&M.votes[0], 256);
+        mbar_init(&M.votes[1], 256);
+        M.again[0][0] = M.again[0][1] = M.again[1][0] = M.again[1][1] = 0;
         mbar_init(&M.qfull, 512);
         mbar_init(&M.fin, 1);
         M.dead = 0;
@@ -240,9 +246,8 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
     if (t_begin < t_end) {
         uint32_t g = M.first;
         unsigned long long t = t_begin;
-        // (the softmax threads hold half a row of scores each, the others little: 4 x 104 + 64 = 5 x 96 registers)
         if (wg == 4) {
-            registers_down<64>();
+            registers_down<kOtherRegs>();
         if (warp == 16) {
             // ---- copies: a lane per page
             uint32_t ks = 0, kp = 0, vs = 0, vp = 0, ring = 0;
@@ -408,18 +413,12 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
             }
         }
         } else {
-            registers_up<104>();
+            registers_up<kSoftmaxRegs>();
             // ---- softmax: two threads a row, 64 of a tile's tokens each
             const uint32_t w = wg / 2u, half = wg % 2u, line = tid % 128u, local = w * 128u + line;       // row of the 128, of the 256
             const uint32_t tS = tmem + w * 128u + half * 64u + ((warp % 4u) * 32u << 16), tO = tmem + 256u + w * 128u + ((warp % 4u) * 32u << 16);
             uint32_t sp = 0, ring = 0;       // phase of sfull[w] (and of ofull[w], one behind)
             auto both = [&]() { asm volatile("bar.sync %0, 256;" ::"r"(1u + w) : "memory"); };      // the row's two threads (and the tile's others)
-            auto either = [&](bool v) {
-                uint32_t r;
-                asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                             : "=r"(r) : "r"((uint32_t)v), "r"(1u + w) : "memory");
-                return r != 0u;
-            };
             while (t < t_end) {
                 Segment s = M.seg[w];
                 to_segment(s, t, g);
@@ -514,7 +513,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                     const float least = M.least[ring];
                     constexpr uint32_t NG = 64 / GS;
                     const float2* scales = &M.scales[ring][half * 4u];
-                    bool rolled;
+                    bool rolled = false;
                     {
                         float x[64];
                         tmem_read32(tS, x);
@@ -561,10 +560,12 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                             R = fmaxf(rt, M.other[w][half ^ 1u][line].x);
                         }
                         const float Rb = R == -INFINITY ? 0.0f : R, mb = mt == -INFINITY ? Rb : mt;
-                        rolled = either(odd || rt > R + kRoom || !(Rb - least - mb <= 80.0f));
-                        if (!rolled) {
-                            l *= exp2_fast(m - mb);
-                            m = mt;
+                        // all 256 threads of the tile have to say so before the weights are handed on; they are asked here and heard when the first
+                        // weights are done (waited for at once, their answer took 290 cycles)
+                        if (odd || rt > R + kRoom || !(Rb - least - mb <= 80.0f)) M.again[w][sp] = 1u;
+                        mbar_arrive_at(bar(M.votes[w]));
+                        {
+                            float sum_l = 0.0f;
                             float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
                             float2 fac2, off2;
 #pragma unroll
@@ -583,15 +584,26 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                                     e.y = exp2_fast(e.y);
                                     pk[i / 2] = pack_half2(e.x, e.y);
                                     sum[i / 2 % 2] = at % GS < 4 ? e : add2(sum[i / 2 % 2], e);
-                                    if (ch == 1 && i == 14) written(0);      // (the stores before are long done)
+                                    if (ch == 1 && i == 14) written(0);      // (the stores before are done)
                                     if (at % GS == GS - 2) {
                                         sum[0] = add2(sum[0], sum[1]);
-                                        l = fmaf(sum[0].x + sum[0].y, exp2_fast(-off2.x - mb), l);
+                                        sum_l = fmaf(sum[0].x + sum[0].y, exp2_fast(-off2.x - mb), sum_l);
                                     }
+                                }
+                                if (ch == 0) {
+                                    // (a barrier of the block's own threads, who all come: waited for whatever else has run out, so that all of
+                                    // them go the same way; tiles in turn have words of their own)
+                                    for (uint32_t n = 0; n < 1u << 20 && !mbar_try(bar(M.votes[w]), sp); n++) {}
+                                    rolled = *(volatile uint32_t*)&M.again[w][sp] != 0u;
+                                    if (rolled) break;
                                 }
                                 tmem_write16(tS + ch * 16u, pk);
                             }
-                            written(1);
+                            if (!rolled) {
+                                l = fmaf(l, exp2_fast(m - mb), sum_l);
+                                m = mt;
+                                written(1);
+                            }
                         }
                     }
                     if (rolled) {
@@ -618,6 +630,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                         M.other[w][half][line].x = rt;
                         both();
                         rt = fmaxf(rt, M.other[w][half ^ 1u][line].x);
+                        if (half == 0u && line == 0u) M.again[w][sp] = 0u;   // (everybody has heard it)
                         both();                                          // (read, before the next is written)
                         if (c == 0) R = -INFINITY;
                         const bool jump = rt > R + kRoom;
