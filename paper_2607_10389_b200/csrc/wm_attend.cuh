@@ -24,8 +24,6 @@ struct AttendArgs {
     wm_pages_report* rep;
 };
 
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 __device__ __forceinline__ void from_float(__nv_bfloat16& o, float v) { o = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void from_float(__half& o, float v) { o = __float2half_rn(v); }
 

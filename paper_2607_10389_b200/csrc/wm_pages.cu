@@ -44,8 +44,8 @@ static bool rows_ok(const wm_rows* r, uint32_t size)
 
 constexpr uint64_t kAppendWarps = 148 * 64;
 // Rows a warp looks at: one while that many warps still fit the GPU a few times over, up to 32 beyond.  Measured, 17,000 rows of
-// prompts in pages of 64, 8 key heads of 128: 24 us with up to 32 rows a warp, 28 with 16, 33 with 8; with one, 73.  Loads of 16 bytes a lane
-// that stay in registers: 8 there (24 us; 4: 25, 16: 24, 32: 29), 4 where a warp looks at one row (256 rows: 3.5 us, with 16 7.7).
+// prompts in pages of 64, 8 key heads of 128: 20 us with up to 32 rows a warp, 22 with 16; with one (and more work a row), 73.  Loads of 16
+// bytes a lane that stay in registers: 8 there (20 us; 4: 21.4, 16: 20.5), 4 where a warp looks at one row (256 rows: 3.5 us, with 16 7.7).
 template <typename T>
 static void append_launch(AppendArgs a, cudaStream_t s)
 {
