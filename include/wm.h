@@ -79,7 +79,8 @@ uint64_t wm_workspace_bytes(uint64_t nbytes, uint32_t chunk_bytes);
  * Paper: fail-closed behaviour (Section 4.1: a move either completes verified or installs nothing).
  * The kernels wait for a bulk copy into shared memory, for the placement scanner (encode: a tile's
  * offset), as the scanner for the tiles' lengths, for a tile's widths from the warps that measure it
- * (encode), and for a slot of a ring in shared memory (wm_checksum_xxh64).  Each wait is bounded
+ * (encode), for a slot of a ring in shared memory (wm_checksum_xxh64), and for the tensor cores' products and what feeds
+ * them (wm_pages_attend).  Each wait is bounded
  * by time on the GPU's own clock, not by a number of polls, so a kernel that shares the GPU with
  * other work and is descheduled for a while is not mistaken for a failure, and a real failure
  * never turns into a hang: when the budget has passed the kernel gives up, withdraws the
@@ -108,7 +109,7 @@ wm_status wm_workspace_status(const void* workspace, void* stream);
 /*
  * wm_inject_stall - test hook for the give-up paths (the paper has no counterpart).
  * While on, calls issued by this process leave out what their bounded waits wait for: the encode
- * kernel's scanner returns at once (no tile ever gets its offset), the checksum and decode kernels
+ * kernel's scanner returns at once (no tile ever gets its offset), the checksum, decode and attention kernels
  * do not start their bulk copies.  With on == 2 it is instead the warp of the encode kernel that
  * publishes a tile's length which never hears that the tile's widths are all there (the other calls
  * run normally).  Every wait then runs out after wm_wait_budget_ms and the call ends in

@@ -70,6 +70,9 @@ __device__ __forceinline__ Request few_request_of(const AttendArgs& a, uint32_t 
 // w (a block; two on an SM) takes tiles w T / W .. (w + 1) T / W.  A unit that ends inside a worker's share is finished there; one that is cut
 // leaves (o, m, R, l) in the workspace, and k_attend_join puts the pieces together in the workers' order (no atomics: the
 // result does not depend on timing).
+//
+// Measured: 64 single rows over 705 MB of codes (8 key heads of 128, groups of 8) 122 us, 5.8 TB/s, 0.89 of the copy rate; one row over
+// 2 MB 9.4 us, of which 5 are the first tile's way (4000 cycles until a block knows its share, the copy, one tile's chain).
 
 template <typename T, int D, int RT> struct Few {
     static constexpr uint32_t kQP = sizeof(T) == 2 && std::is_same<T, __half>::value ? 3 : 2;     // pieces of a query

@@ -19,6 +19,10 @@ namespace wm {
 // (weights lie in f16 from 2 on downwards, so up to 2^15 there is room), which makes rescaling O in tensor memory rare: a warp that does it
 // holds up the other three of its tile for 900 cycles, and with jumps of 2^7 one of them did in every other tile.
 // Work is dealt out as in the kernel for few rows: equal shares of tiles, units cut between workers are joined in order.
+//
+// Measured: four prompts' 1024 rows over 5000 to 9000 tokens (32 heads, 8 key heads of 128; 437 GFLOP) 393 us, 1.11 PFLOP/s, 0.68 of the
+// bf16 rate in short runs, 445 us in runs of seconds.  A pair of tiles takes 3400 cycles; the tensor cores need 2048 of them and the
+// exponentials 2130, but a tile's scores, softmax, weights and outputs follow one another, and only two tiles fit in tensor memory.
 
 // A worker's segments: consecutive tiles of one unit.  base, end: the first tile of its group's first key head, and behind its last's.
 struct Segment {
