@@ -17,7 +17,7 @@ struct AttendArgs {
     float* lse;
     uint32_t n_rows, q_heads, group;
     float scale;
-    uint32_t causal, window;
+    uint32_t causal, window;    // window: below 2^30, 0 for none
     uint32_t few_rows;          // requests with more rows (times heads that share a key head) are the kernel's for many
     unsigned char* ws;
     uint32_t wait_ns, inject;
@@ -131,7 +131,7 @@ template <int RT> __device__ __forceinline__ UnitShape shape_of(const AttendArgs
 {
     UnitShape u;
     u.row_tiles = ((uint32_t)r.rows * a.group + RT - 1u) / RT;
-    const int32_t lo = a.window ? max(0, r.kv - r.rows + 1 - (int32_t)min(a.window, 0x7FFFFFFFu)) : 0;
+    const int32_t lo = a.window ? max(0, r.kv - r.rows + 1 - (int32_t)a.window) : 0;
     u.j0 = (uint32_t)lo / 128u;
     const uint32_t end = ((uint32_t)r.kv + 127u) / 128u;
     u.nt = end > u.j0 ? end - u.j0 : 1u;
@@ -146,7 +146,7 @@ template <int D> __device__ __forceinline__ uint32_t swizzled(uint32_t at) { ret
 struct Span {
     int32_t any_lo, any_hi, all_lo, all_hi;
 };
-__device__ __forceinline__ int32_t sees_from(const AttendArgs& a, int32_t pos) { return a.window ? max(0, pos + 1 - (int32_t)min(a.window, 0x7FFFFFFFu)) : 0; }
+__device__ __forceinline__ int32_t sees_from(const AttendArgs& a, int32_t pos) { return a.window ? max(0, pos + 1 - (int32_t)a.window) : 0; }
 __device__ __forceinline__ int32_t sees_to(const AttendArgs& a, int32_t kv, int32_t pos) { return a.causal ? min(kv, max(0, pos + 1)) : kv; }
 __device__ __forceinline__ Span span_of(const AttendArgs& a, int32_t kv, int32_t pos0, int32_t pos1)
 {

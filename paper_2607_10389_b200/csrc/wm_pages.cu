@@ -185,9 +185,10 @@ wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows
     uint32_t shift = 0;
     if (type < WM_TYPE_BF16 || type > WM_TYPE_F32) return WM_ERR_ARG;
     const uint32_t size = type == WM_TYPE_F32 ? 4 : 2;
-    if (!pages_ok(pages, shift) || !rows_ok(k, size) || !rows_ok(v, size) || !slots || n_rows >= (1u << 24)) return WM_ERR_ARG;
+    if (!pages_ok(pages, shift) || !k || !v || n_rows >= (1u << 24)) return WM_ERR_ARG;
     g_launches = 0;
     if (n_rows == 0) return WM_OK;
+    if (!rows_ok(k, size) || !rows_ok(v, size) || !slots) return WM_ERR_ARG;
     const AppendArgs a = {*pages, shift, {k->ptr, v->ptr}, {k->row_stride, v->row_stride}, {k->head_stride, v->head_stride}, slots, n_rows, 1, report};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (type == WM_TYPE_BF16) append_launch<__nv_bfloat16>(a, s);
@@ -208,7 +209,7 @@ wm_status wm_pages_attend(const wm_pages* pages, const int32_t* table, uint32_t 
                           void* workspace, uint64_t workspace_bytes, wm_pages_report* report, void* stream)
 {
     uint32_t shift = 0;
-    if (!pages_ok(pages, shift) || !rows_ok(q, 2) || !rows_ok(out, 2) || !table || !kv_len || !q_start) return WM_ERR_ARG;
+    if (!pages_ok(pages, shift) || !q || !out || !table || !kv_len || !q_start) return WM_ERR_ARG;
     if ((type != WM_TYPE_BF16 && type != WM_TYPE_F16) || (options & ~WM_ATTEND_CAUSAL) || (window && !(options & WM_ATTEND_CAUSAL))) return WM_ERR_ARG;
     if (n_requests == 0 || n_requests > kMaxRequests || table_stride == 0 || (uint64_t)n_requests * table_stride >= (1ull << 31)) return WM_ERR_ARG;
     if ((uint64_t)table_stride << shift > (1ull << 30) || n_rows >= (1u << 24) || max_q == 0 || !std::isfinite(scale)) return WM_ERR_ARG;
@@ -217,6 +218,8 @@ wm_status wm_pages_attend(const wm_pages* pages, const int32_t* table, uint32_t 
     if (!workspace || !aligned16(workspace) || workspace_bytes < wm_pages_workspace_bytes(pages->head_dim)) return WM_ERR_ARG;
     g_launches = 0;
     if (n_rows == 0) return WM_OK;
+    if (!rows_ok(q, 2) || !rows_ok(out, 2)) return WM_ERR_ARG;
+    if (window >= (1u << 30)) window = 0;             // (no request is longer: such a window hides nothing)
     const AttendArgs a = {*pages, shift, table, table_stride, kv_len, q_start, n_requests, q->ptr, out->ptr, q->row_stride, q->head_stride,
                           out->row_stride, out->head_stride, lse, n_rows, q_heads, q_heads / pages->kv_heads, scale,
                           options & WM_ATTEND_CAUSAL, window, 0u, static_cast<unsigned char*>(workspace), wait_budget_ns(), inject_bits(), report};

@@ -673,6 +673,55 @@ def test_calls_refuse_tensors_of_another_device(monkeypatch):
 
 
 @gpu
+@pytest.mark.parametrize("window", [1, 2 ** 30 - 1, 2 ** 30, 2 ** 31 - 1, 2 ** 32 - 1])
+@pytest.mark.parametrize("lens,rows", [([5, 300, 0], [9, 2, 3]), ([100, 300, 0], [200, 150, 40])])
+def test_attend_with_windows_of_any_size_and_more_rows_than_tokens(window, lens, rows):
+    g = torch.Generator().manual_seed(27)
+    pages, arrays, table = _attend_case(lens, 32, 1, 64, g)
+    _attend(pages, arrays, table, lens, rows, 2, torch.bfloat16, g, window=window)
+
+
+@gpu
+def test_calls_on_no_rows():
+    pages, none = wm.new_pages(4, 16, 2, 64), torch.zeros(0, 2, 64, device="cuda", dtype=torch.bfloat16)
+    wm.wm_pages_append(pages, none, none, _dev([]))
+    wm.wm_pages_attend(pages, _dev([[0, 1]]), _dev([3]), _dev([0, 0]), none, none.clone(), wm.new_pages_workspace(64), max_q=1)
+    count, start = _dev([4]), _dev([9, 9])
+    wm.wm_pages_plan(_dev([3]), _dev([3]), 16, _dev([[0, 1]]), _dev([0, 1, 2, 3]), count, count, start, _dev([]))
+    torch.cuda.synchronize()
+    assert count.item() == 4 and start.tolist() == [0, 0] and not pages.k.any()
+
+
+@gpu
+def test_attention_beside_the_movers_calls_on_another_stream():
+    """The encoder takes a whole SM's shared and tensor memory, so blocks of the two take turns; neither waits for the other."""
+    g = torch.Generator().manual_seed(28)
+    lens = [900, 3000, 1500]
+    pages, arrays, table = _attend_case(lens, 64, 4, 128, g)
+    tab, kv = _dev(table), _dev(lens)
+    n, chunk = 4 << 20, 65536
+    cache = torch.randn(n // 2, generator=g).to(torch.bfloat16).cuda()
+    mover = [torch.cuda.Stream() for _ in range(2)]
+    scratch, res, crc = wm.new_workspace(n, chunk), wm.new_result(), torch.zeros(n // chunk, dtype=torch.int32, device="cuda")
+    wires = [torch.zeros(wm.wire_bound(n, chunk), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    wm.wm_encode(cache, chunk, None, crc, wires[0], scratch, res)
+    length = wm.read_result(res).wire_len
+    for rows in ([1, 1, 1], [300, 400, 100]):
+        starts = [0, rows[0], rows[0] + rows[1], sum(rows)]
+        q = torch.randn((sum(rows), 16, 128), generator=g).to(torch.bfloat16).cuda()
+        want, out, ws = torch.zeros_like(q), torch.zeros_like(q), wm.new_pages_workspace(128)
+        start = _dev(starts)
+        wm.wm_pages_attend(pages, tab, kv, start, q, want, ws, max_q=max(rows))
+        torch.cuda.synchronize()
+        for _ in range(20):
+            wm.wm_pages_attend(pages, tab, kv, start, q, out, ws, max_q=max(rows), stream=mover[0])
+            wm.wm_encode(cache, chunk, None, crc, wires[1], scratch, res, stream=mover[1])
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        assert wm.read_result(res).ok and torch.equal(wires[0][:length], wires[1][:length])
+
+
+@gpu
 def test_many_slots_at_an_address_that_is_not_aligned():
     n, page = 40, 16
     r = random.Random(4)
