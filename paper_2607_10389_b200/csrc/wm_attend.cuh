@@ -221,6 +221,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
         M.dead = 0;
         M.poison = 0;
     }
+    if (tid == 32) { fetch_map(&kmap); fetch_map(&vmap); }
     if (warp == 4) tmem_alloc<F::kCols>((uint32_t)__cvta_generic_to_shared(&M.tmem));
     grid_dep_wait();
     grid_dep_launch();

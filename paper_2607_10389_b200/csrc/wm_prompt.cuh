@@ -210,6 +210,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
         M.dead = 0;
         M.nan_seen = 0;
     }
+    if (tid == 32) { fetch_map(&kmap); fetch_map(&vmap); }
     if (warp == 16) tmem_alloc<512>((uint32_t)__cvta_generic_to_shared(&M.tmem));
     grid_dep_wait();
     grid_dep_launch();
