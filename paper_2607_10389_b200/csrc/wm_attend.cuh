@@ -578,16 +578,24 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                             for (uint32_t i = 0; i < D; i += 16)
                                 asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v0 + tid * D + i), "r"(0u) : "memory");
                         } else if (!all) {
-                            uint32_t found = 0;
+                            uint32_t found = 0;           // a byte of 0x7F without its sign carries into bit 7 when one is added
 #pragma unroll
-                            for (uint32_t i = 0; i < D; i += 4) {
-                                const uint32_t at = v0 + swizzled<D>(tid * D + i), v = lds_now<0>(at);
-                                const uint32_t is = __vcmpeq4(v & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
-                                if (is) {
-                                    found = 1;
-                                    sts_now(at, v & ~is);
-                                    nan_at[i / 32] |= ((is & 1u) | (is >> 7 & 2u) | (is >> 14 & 4u) | (is >> 21 & 8u)) << (i % 32);
-                                }
+                            for (uint32_t i = 0; i < D; i += 16) {
+                                const uint4 v = lds16(v0 + swizzled<D>(tid * D + i));
+                                found |= ((v.x & 0x7F7F7F7Fu) + 0x01010101u) | ((v.y & 0x7F7F7F7Fu) + 0x01010101u) | ((v.z & 0x7F7F7F7Fu) + 0x01010101u) |
+                                         ((v.w & 0x7F7F7F7Fu) + 0x01010101u);
+                            }
+                            found &= 0x80808080u;
+                            if (found) {
+#pragma unroll
+                                for (uint32_t k = 0; k < D / 32; k++)
+#pragma unroll 1
+                                    for (uint32_t i = 0; i < 32; i += 4) {
+                                        const uint32_t at = v0 + swizzled<D>(tid * D + 32u * k + i), v = lds_now<0>(at);
+                                        const uint32_t is = __vcmpeq4(v & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                                        sts_now(at, v & ~is);
+                                        nan_at[k] |= ((is & 1u) | (is >> 7 & 2u) | (is >> 14 & 4u) | (is >> 21 & 8u)) << i;
+                                    }
                             }
                             if (found) M.poison = 1u;
                         }
@@ -648,13 +656,22 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                         tmem_read8(lane_t + F::cL + 8u * g, l);
                         tmem_wait_loads();
                     }
+                    // eight sums over 32 lanes: halves of the rows change hands with the lanes, so that nine exchanges do instead of forty
+                    float v[8];
 #pragma unroll
-                    for (uint32_t i = 0; i < 8; i++) {
-                        float v = l[i];
+                    for (uint32_t i = 0; i < 8; i++) v[i] = l[i];
 #pragma unroll
-                        for (uint32_t d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-                        if (lane == i) M.sum[warp][8u * g + i] = v;
+                    for (uint32_t n = 4; n; n >>= 1) {
+                        const bool upper = lane & (4u * n);
+#pragma unroll
+                        for (uint32_t i = 0; i < n; i++) {
+                            const float give = upper ? v[i] : v[n + i], keep = upper ? v[n + i] : v[i];
+                            v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, 4 * n);
+                        }
                     }
+                    v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], 2);
+                    v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], 1);
+                    if (lane % 4u == 0u) M.sum[warp][8u * g + lane / 4u] = v[0];
                 }
                 if (lane < RT) *reinterpret_cast<float2*>(M.state[warp][lane]) = make_float2(m_run, r_run);
                 asm volatile("bar.sync 1, 128;" ::: "memory");
