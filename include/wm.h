@@ -532,7 +532,8 @@ wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows
  *   max_q     the most rows any request has, as far as the caller knows (1: a step of single tokens).  It
  *             chooses the kernels; requests with more rows are answered all the same, more slowly
  *   options   WM_ATTEND_CAUSAL or 0
- *   workspace [dev] wm_pages_workspace_bytes(head_dim) bytes, 16-byte aligned, contents arbitrary
+ *   workspace [dev] wm_pages_workspace_bytes(head_dim) bytes, 16-byte aligned, contents arbitrary.  One call's at a time:
+ *             calls (or captured graphs) that may run side by side need one each
  *   report    [dev] or NULL.  WM_ERR_ARG with the lowest request concerned: a negative length, a length beyond its row of
  *             the table, row numbers that decrease or lie outside 0 .. n_rows (its rows are left as they are), or
  *             a page number outside the pool (rows that see it get NaN).  WM_ERR_TIMEOUT: a wait ran out (see

@@ -100,7 +100,7 @@ template <typename T, int D, int RT> struct Few {
         unsigned long long first_prefix;
         int2 span[RT];                    // the tokens a row sees: from, to
         Request first;
-        uint32_t first_req, tmem, dead, poison;
+        uint32_t first_req, tmem, dead;
     };
     static constexpr uint32_t kSmem = oMisc + (uint32_t)sizeof(Misc) + 1024;
 };
@@ -166,6 +166,14 @@ __device__ __forceinline__ void store_joined(const AttendArgs& a, const Request&
     if (d == 0 && a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
+// Whether `p` holds in any of the 128 threads that have the softmax.
+__device__ __forceinline__ bool any_of_128(bool p)
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"((uint32_t)p) : "memory");
+    return r != 0u;
+}
+
 // What a lane of the copying warp needs of a tile: its page (lane = page of the tile) and that page's scales.  They are asked for
 // ahead, the page two tiles and the scales one: one after the other in front of every copy they took longer than the tile.
 struct PageOf {
@@ -219,7 +227,6 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
         mbar_init(&M.pbar, 128);
         mbar_init(&M.fin, 1);
         M.dead = 0;
-        M.poison = 0;
     }
     if (tid == 32) { fetch_map(&kmap); fetch_map(&vmap); }
     if (warp == 4) tmem_alloc<F::kCols>((uint32_t)__cvta_generic_to_shared(&M.tmem));
@@ -566,7 +573,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                     }
                     // values that not every row sees must not meet the others' zero weights as NaN: tokens that no row sees are cleared,
                     // NaN codes of tokens that some rows see are taken out and put into those rows' outputs below
-                    uint32_t nan_at[D / 32];
+                    uint32_t nan_at[D / 32], found = 0;
                     if (!whole) {
                         mbar_wait(bar(M.vfull[stage]), kphase, a.wait_ns, &M.dead);
                         const uint32_t v0 = base_s + stage * F::kStage + F::kHalf;
@@ -578,7 +585,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                             for (uint32_t i = 0; i < D; i += 16)
                                 asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v0 + tid * D + i), "r"(0u) : "memory");
                         } else if (!all) {
-                            uint32_t found = 0;           // a byte of 0x7F without its sign carries into bit 7 when one is added
+                            // a byte of 0x7F without its sign carries into bit 7 when one is added
 #pragma unroll
                             for (uint32_t i = 0; i < D; i += 16) {
                                 const uint4 v = lds16(v0 + swizzled<D>(tid * D + i));
@@ -597,7 +604,6 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                                         nan_at[k] |= ((is & 1u) | (is >> 7 & 2u) | (is >> 14 & 4u) | (is >> 21 & 8u)) << i;
                                     }
                             }
-                            if (found) M.poison = 1u;
                         }
                     }
                     async_proxy_fence();
@@ -607,10 +613,11 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                     mbar_wait(bar(M.obar), ophase, a.wait_ns, &M.dead);
                     ophase ^= 1u;
                     tmem_fence_after_sync();
-                    const bool poison = *(volatile uint32_t*)&M.poison != 0u;
+                    // (asked of all threads at one barrier: they have to agree even where a wait ran out and some are ahead)
+                    const bool poison = !whole && any_of_128(found != 0u);
                     if (poison) {                          // rare: the marks through P's memory (its MMAs are done)
 #pragma unroll
-                        for (uint32_t i = 0; i < D / 32; i++) sts_now(ps + tid * 16u + 4u * i, whole ? 0u : nan_at[i]);
+                        for (uint32_t i = 0; i < D / 32; i++) sts_now(ps + tid * 16u + 4u * i, nan_at[i]);
                         asm volatile("bar.sync 1, 128;" ::: "memory");
                     }
 #pragma unroll 1
@@ -640,11 +647,6 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                         if (G8 > 1) tmem_write8(lane_t + F::cA + 8u * g, o);
                     }
                     if (G8 > 1) tmem_wait_stores();
-                    if (poison) {
-                        asm volatile("bar.sync 1, 128;" ::: "memory");
-                        if (tid == 0) M.poison = 0;
-                        asm volatile("bar.sync 1, 128;" ::: "memory");
-                    }
                     if (++stage == F::kStages) { stage = 0; kphase ^= 1u; }
                 }
 

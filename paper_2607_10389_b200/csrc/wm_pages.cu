@@ -31,6 +31,8 @@ static bool pages_ok(const wm_pages* p, uint32_t& shift)
     if (((p->page_stride | p->head_stride | p->token_stride) & 15u) != 0) return false;
     shift = p->page_tokens == 16 ? 4 : p->page_tokens == 32 ? 5 : p->page_tokens == 64 ? 6 : p->page_tokens == 128 ? 7 : 0;
     if (!shift || (p->head_dim != 64 && p->head_dim != 128)) return false;
+    if (((p->page_stride | p->head_stride | p->token_stride) >> 40) != 0) return false;
+    if ((p->kv_heads > 1 && p->head_stride < p->head_dim) || (p->n_pages > 1 && p->page_stride < p->head_dim)) return false;    // shared bytes
     if (p->token_stride < p->head_dim || p->kv_heads == 0 || p->kv_heads > 1024) return false;
     if (p->n_pages == 0 || (uint64_t)p->n_pages * p->page_tokens >= (1ull << 31)) return false;
     return true;

@@ -32,6 +32,7 @@ def _c_rows(**change):
 
 
 BAD_PAGES = [dict(k=None), dict(v_scale=None), dict(k=8 + (1 << 20)), dict(page_stride=24), dict(token_stride=64), dict(token_stride=136),
+             dict(page_stride=1 << 40), dict(token_stride=1 << 40), dict(page_stride=0), dict(head_stride=64),
              dict(n_pages=0), dict(n_pages=1 << 25), dict(page_tokens=8), dict(page_tokens=48), dict(page_tokens=256), dict(kv_heads=0),
              dict(kv_heads=1025), dict(head_dim=96), dict(head_dim=0)]
 
@@ -610,6 +611,35 @@ def test_attend_whose_waits_run_out_reports_it_gives_nan_and_the_next_call_is_ri
     assert report[0] == "ERR_TIMEOUT"
     assert out.isnan().all() and lse.isnan().all()
     _attend(pages, arrays, table, lens, rows, 4, torch.bfloat16, g, q=q)
+
+
+@gpu
+@pytest.mark.parametrize("rows", [[1, 1, 1], [2, 5, 3], [8, 7, 4], [200, 140, 130]])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attend_whose_waits_run_out_where_the_tiles_memory_holds_nan_codes(rows, dim):
+    """Tiles that never came are looked through for NaN all the same, by threads that are no longer in step: what was in
+    their memory before must not send them different ways."""
+    g = torch.Generator().manual_seed(20)
+    lens = [300, 140, 131]
+    pages, arrays, table = _attend_case(lens, 64, 2, dim, g)
+    q = torch.randn((sum(rows), 4, dim), generator=g)
+    want = _attend(pages, arrays, table, lens, rows, 4, torch.bfloat16, g, q=q)
+    kept = pages.v.clone()
+    for _ in range(5):
+        pages.v.view(torch.uint8).fill_(0x7F)
+        out = _attend(pages, arrays, table, lens, rows, 4, torch.bfloat16, g, q=q, check=False)[0]
+        assert out.isnan().all()
+        wm.wait_budget_ms(20)
+        wm.inject_stall(1)
+        try:
+            out, lse, report = _attend(pages, arrays, table, lens, rows, 4, torch.bfloat16, g, q=q, check=False)
+        finally:
+            wm.inject_stall(0)
+            wm.wait_budget_ms(2000)
+        assert report[0] == "ERR_TIMEOUT" and out.isnan().all() and lse.isnan().all()
+    pages.v.copy_(kept)
+    got = _attend(pages, arrays, table, lens, rows, 4, torch.bfloat16, g, q=q)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
 @gpu
