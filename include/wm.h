@@ -526,7 +526,8 @@ wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows
  * left as they are.  Codes a row does not see do not touch it, whatever they hold (NaN included).
  *   table     [dev] i32[n_requests][table_stride], table_stride * page_tokens <= 2^30; kv_len [dev] i32[n_requests];
  *             q_start [dev] i32[n_requests + 1]
- *   q, out    n_rows rows of q_heads heads of the pool's head_dim, WM_TYPE_BF16 or WM_TYPE_F16; must not overlap
+ *   q, out    n_rows rows of q_heads heads of the pool's head_dim, WM_TYPE_BF16 or WM_TYPE_F16; must not overlap, nor may
+ *             two elements of out
  *   lse       [dev] f32[n_rows][q_heads] or NULL
  *   q_heads   a multiple of kv_heads, at most 64 * kv_heads; n_rows * q_heads / kv_heads <= 2^24
  *   max_q     the most rows any request has, as far as the caller knows (1: a step of single tokens).  It

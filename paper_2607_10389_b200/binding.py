@@ -565,6 +565,8 @@ def wm_pages_attend(pages: Pages, table: torch.Tensor, kv_len: torch.Tensor, q_s
     here, n, shape, dim = _here(), kv_len.numel(), q.shape, pages.head_dim
     if len(shape) != 3 or out.dtype is not q.dtype or out.shape != shape:
         raise WmError("q must be (rows, heads, channels) and out have its type and shape")
+    if window < 0 or (max_q is not None and max_q < 0):
+        raise WmError("window and max_q must not be negative")
     rows, heads, _ = shape
     if lse is not None and not (lse.dtype is torch.float32 and lse.get_device() == here and lse.shape == (rows, heads) and lse.is_contiguous()):
         _refuse(lse, "lse", here)

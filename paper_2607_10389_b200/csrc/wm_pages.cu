@@ -221,6 +221,7 @@ wm_status wm_pages_attend(const wm_pages* pages, const int32_t* table, uint32_t 
     g_launches = 0;
     if (n_rows == 0) return WM_OK;
     if (!rows_ok(q, 2) || !rows_ok(out, 2)) return WM_ERR_ARG;
+    if ((n_rows > 1 && out->row_stride < pages->head_dim) || (q_heads > 1 && out->head_stride < pages->head_dim)) return WM_ERR_ARG;
     if (window >= (1u << 30)) window = 0;             // (no request is longer: such a window hides nothing)
     const AttendArgs a = {*pages, shift, table, table_stride, kv_len, q_start, n_requests, q->ptr, out->ptr, q->row_stride, q->head_stride,
                           out->row_stride, out->head_stride, lse, n_rows, q_heads, q_heads / pages->kv_heads, scale,

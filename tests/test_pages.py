@@ -1,5 +1,6 @@
 """The paged 8-bit cache: block tables from lengths, new tokens in 8 bits, attention over the pool."""
 import ctypes
+import types
 import random
 
 import pytest
@@ -65,6 +66,7 @@ def test_append_of_no_rows_launches_nothing():
                                     dict(type=2), dict(rows=1 << 24), dict(q_heads=0), dict(q_heads=12), dict(q_heads=8 * 65), dict(max_q=0),
                                     dict(scale=float("nan")), dict(scale=float("inf")), dict(options=2), dict(options=0, window=5),
                                     dict(ws=None), dict(ws=8), dict(ws_bytes=16), dict(q=dict(row_stride=4)), dict(o=dict(ptr=2)),
+                                    dict(o=dict(row_stride=0), rows=2), dict(o=dict(head_stride=64)),
                                     dict(q=dict(ptr=None))], ids=str)
 def test_attend_refuses_bad_arguments(change):
     at, p = 1 << 20, _c_pages()
@@ -92,6 +94,14 @@ def test_plan_refuses_bad_arguments(change):
     g = lambda name, other: change.get(name, other)  # noqa: E731
     assert wm.lib().wm_pages_plan(g("old", at), at, g("n", 1), g("page", 64), g("pool", 10), at, g("stride", 4) & 0xFFFFFFFF, g("free", at),
                                   g("count", at), at, g("start", at), g("slots", at), g("n_slots", 5) & 0xFFFFFFFF, None, None) == -1
+
+
+def test_the_binding_refuses_negative_windows_and_rows():
+    q = torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    i = torch.zeros(2, dtype=torch.int32)
+    for what in (dict(window=-1), dict(max_q=-1)):
+        with pytest.raises(wm.WmError, match="negative"):
+            wm.wm_pages_attend(types.SimpleNamespace(head_dim=64), i[None], i[:1], i, q, torch.empty_like(q), q, **what)
 
 
 def test_the_binding_refuses_host_tensors():
