@@ -72,7 +72,7 @@ __device__ __forceinline__ Request few_request_of(const AttendArgs& a, uint32_t 
 // result does not depend on timing).
 //
 // Measured: 64 single rows over 705 MB of codes (8 key heads of 128, groups of 8) 122 us, 5.8 TB/s, 0.89 of the copy rate; one row over
-// 2 MB 9.4 us, of which 5 are the first tile's way (4000 cycles until a block knows its share, the copy, one tile's chain).
+// 2 MB 9.5 us, of which 5 are the first tile's way (4000 cycles until a block knows its share, the copy, one tile's chain).
 
 template <typename T, int D, int RT> struct Few {
     static constexpr uint32_t kQP = sizeof(T) == 2 && std::is_same<T, __half>::value ? 3 : 2;     // pieces of a query
