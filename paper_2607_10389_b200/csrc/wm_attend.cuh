@@ -534,7 +534,8 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                         const float mb = mt == -INFINITY ? 0.0f : mt, rb = mr == -INFINITY ? 0.0f : mr, ob = mo == -INFINITY ? 0.0f : mo;
                         // what exponents refer to, and the factors of l, of o and of this tile's outputs
                         *reinterpret_cast<float4*>(M.state[warp][lane]) = make_float4(mb, ob - 8.0f, exp2_fast(m_run - mb), exp2_fast(r_run - rb));
-                        M.sum[warp][lane] = exp2_fast(ob - 8.0f - rb);
+                        // (no outputs from a tile of which the row sees nothing: its ob stands for nothing, and 2^(ob - rb) may be infinite)
+                        M.sum[warp][lane] = mo == -INFINITY ? 0.0f : exp2_fast(ob - 8.0f - rb);
                         m_run = mt;
                         r_run = mr;
                     }
