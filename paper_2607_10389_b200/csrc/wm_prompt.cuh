@@ -493,7 +493,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                     both();
                     if (half == 0u && line == 0u) M.seg[w] = s;       // (read again when the unit's part ends: in registers it would cost the loop)
                 }
-                const float f = M.f[local];
+                const float f = live && lo < hi ? M.f[local] : 1.0f;      // (a row that sees nothing: whatever its query is)
                 float m = -INFINITY, l = 0.0f, R = -INFINITY;       // R: what O refers to
                 const uint32_t count = s.count;
                 for (uint32_t c = 0; c < count; c++, t0 += 128) {
@@ -516,7 +516,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                         const float2 first = scales[0];
                         auto scale = [&](uint32_t i) { return NG == 1 ? first : scales[i * (GS / 16)]; };       // of group i: (key scale, log2 of the value scale)
                         tmem_wait_loads();
-                        bool odd = false;       // a factor that is not positive would turn what is masked into NaN
+                        bool odd = false;       // a factor that is not positive, or whose product is not, would turn what is masked into NaN (f is, in a row that is NaN anyway)
                         if (!whole) {
 #pragma unroll
                             for (uint32_t ch = 0; ch < 2; ch++) {
@@ -527,7 +527,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                                     if (!(seen >> i & 1u)) x[32 * ch + i] = -INFINITY;
                             }
 #pragma unroll
-                            for (uint32_t i = 0; i < NG; i++) odd = odd || !(scale(i).x > 0.0f) || a.scale == 0.0f;
+                            for (uint32_t i = 0; i < NG; i++) odd = odd || !(scale(i).x > 0.0f) || scale(i).x * f == 0.0f;
                         }
                         // the largest score and the largest weighted score
                         float mt = m, rt = -INFINITY;

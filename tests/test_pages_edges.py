@@ -72,3 +72,62 @@ def test_attend_drafts_across_a_tile_s_border_with_low_scores(dtype, group, scor
     want = ref64.attend(pages.k, pages.v, pages.k_scale, pages.v_scale, table, lens, starts, q, 64 ** -0.5, True, 0)
     far, far_lse = ref.bounds(*want, dtype, 64)
     assert ((out.double() - want[0]).abs() <= far).all() and ((lse.double() - want[1]).abs() <= far_lse).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("rows", [[3, 2], [200, 131]])
+@pytest.mark.parametrize("dim,page,group", [(64, 16, 1), (128, 64, 4)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 100), (False, 0)])
+def test_attend_queries_of_zeros_over_keys_of_zeros(dtype, rows, dim, page, group, causal, window):
+    """Factors of scores that are not there any more in 32 bits: zero or tiny queries, keys under the smallest scale
+    (as wm_pages_append writes zeros), a tiny softmax scale; ordinary values and zeros."""
+    g = torch.Generator().manual_seed(32)
+    lens = [300, 131]
+    pages, arrays, table = tp._attend_case(lens, page, 2, dim, g)
+    q = torch.randn((sum(rows), 2 * group, dim), generator=g)
+    q[::3] = 0.0
+    q[1::3] *= 2.0 ** -20
+    run = lambda **kw: tp._attend(pages, arrays, table, lens, rows, 2 * group, dtype, g, causal, window, q=q, **kw)  # noqa: E731
+    run()
+    run(scale=2.0 ** -120)
+    arrays[2][::2] = 2.0 ** -126                         # codes of any size under it, then zeros everywhere
+    pages.k_scale.copy_(arrays[2])
+    run()
+    arrays[0].zero_(), arrays[2].fill_(2.0 ** -126)
+    pages.k.copy_(arrays[0]), pages.k_scale.copy_(arrays[2])
+    run()
+    arrays[1].zero_(), arrays[3].fill_(2.0 ** -126)
+    pages.v.copy_(arrays[1]), pages.v_scale.copy_(arrays[3])
+    run()
+
+
+@gpu
+@pytest.mark.parametrize("rows", [5, 150])
+def test_a_prompt_of_zeros_through_append_and_attend(rows):
+    """What an engine warms up with."""
+    pages = wm.new_pages(8, 64, 2, 128)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    table, count, start, slots = i32([[-1] * 4]), i32([8]), i32([0, 0]), i32([0] * rows)
+    wm.wm_pages_plan(i32([0]), i32([rows]), 64, table, i32(list(range(8))), count, count, start, slots)
+    kv = torch.zeros(rows, 2, 128, device="cuda", dtype=torch.bfloat16)
+    q = torch.zeros(rows, 8, 128, device="cuda", dtype=torch.bfloat16)
+    wm.wm_pages_append(pages, kv, kv + 0.5, slots)
+    out, lse = torch.full_like(q, 7.0), torch.full((rows, 8), 7.0, device="cuda")
+    wm.wm_pages_attend(pages, table, i32([rows]), start, q, out, wm.new_pages_workspace(128), lse=lse, max_q=rows)
+    assert (out == 0.5).all()                            # 0.5 is a code under a power of two, and so is their mean
+    want = torch.arange(1, rows + 1, dtype=torch.float64).log()[:, None]
+    assert ((lse.cpu().double() - want).abs() <= 2.0 ** -18 + 2.0 ** -22 * want).all()
+
+
+@gpu
+@pytest.mark.parametrize("rows", [12, 150])
+def test_attend_rows_that_see_nothing_give_zeros_whatever_their_queries_are(rows):
+    g = torch.Generator().manual_seed(33)
+    lens = [rows - 5]
+    pages, arrays, table = tp._attend_case(lens, 32, 2, 64, g)
+    q = torch.randn((rows, 2, 64), generator=g)
+    q[0], q[1, 0, 3], q[2, 1, 5], q[3], q[4] = float("nan"), float("inf"), -float("inf"), 0.0, 2.0 ** -24
+    for dtype in HALVES:
+        out, lse = tp._attend(pages, arrays, table, lens, [rows], 2, dtype, g, q=q)
+        assert (out[:5] == 0).all() and (lse[:5] == -float("inf")).all()
