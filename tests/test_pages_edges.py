@@ -131,3 +131,65 @@ def test_attend_rows_that_see_nothing_give_zeros_whatever_their_queries_are(rows
     for dtype in HALVES:
         out, lse = tp._attend(pages, arrays, table, lens, [rows], 2, dtype, g, q=q)
         assert (out[:5] == 0).all() and (lse[:5] == -float("inf")).all()
+
+
+def _attend_large(kv_heads, group, dim, page, dtype, lens, rows, causal, window, g, max_q=None, rise=0.0, n_rows_more=3):
+    """Against 64 bits on the GPU.  `rise`: how far scores climb from the first token to the last."""
+    pages, arrays, table = tp._attend_case(lens, page, kv_heads, dim, g, spread=3)
+    heads, n = kv_heads * group, sum(rows)
+    q = torch.randn((n + n_rows_more, heads, dim), generator=g)
+    if rise:
+        q = 1.0 + 0.25 * q
+        for i, x in enumerate(lens):
+            for j, p in enumerate(table[i][:ref.pages_of(x, page)]):
+                t = (j * page + torch.arange(page)) / x
+                y = t[None, :, None] * rise * dim ** -0.5 + 0.1 * torch.randn((kv_heads, page, dim), generator=g)
+                s = 2.0 ** torch.ceil(torch.log2(y.abs().amax((1, 2)) / 448.0))
+                arrays[0][p], arrays[2][p] = (y / s[:, None, None]).to(ref.E4M3).view(torch.uint8), s
+        pages.k.copy_(arrays[0]), pages.k_scale.copy_(arrays[2])
+    q = q.to(dtype).cuda()
+    starts = [0]
+    for r in rows:
+        starts.append(starts[-1] + r)
+    out, lse, ws, report = torch.full_like(q, 7.0), torch.full((q.shape[0], heads), 7.0, device="cuda"), wm.new_pages_workspace(dim), wm.new_pages_report()
+    ws.fill_(0xFF)
+    wm.wm_pages_attend(pages, tp._dev(table), tp._dev(lens), tp._dev(starts), q, out, ws, lse=lse, causal=causal, window=window,
+                       max_q=max_q or max(rows), report=report)
+    assert wm.read_pages_report(report) == ("OK", None)
+    assert (out[n:] == 7).all() and (lse[n:] == 7).all()
+    want = ref64.attend(pages.k, pages.v, pages.k_scale, pages.v_scale, table, lens, starts, q[:n], dim ** -0.5, causal, window)
+    far, far_lse = ref.bounds(*want, dtype, dim)
+    off, off_lse = (out[:n].double() - want[0]).abs(), (lse[:n].double() - want[1]).abs()
+    assert (off <= far).all(), (off / far).max()
+    fine = ~want[1].isinf()
+    assert torch.equal(lse[:n].isinf(), want[1].isinf()) and (off_lse[fine] <= far_lse[fine]).all(), (off_lse / far_lse)[fine].max()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("dim,page", [(64, 64), (128, 16), (128, 128), (64, 32)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 700), (False, 0)])
+@pytest.mark.parametrize("rise", [0.0, 60.0])
+def test_attend_prompts_of_many_tiles_a_block(dtype, dim, page, causal, window, rise):
+    """Some 2000 tiles for the GPU's 148 blocks: units of many tiles, several units a block, parts of many tiles; with scores that
+    climb by 60 (86 in powers of two), so that what outputs refer to moves on the way."""
+    g = torch.Generator().manual_seed(36)
+    _attend_large(8, 4, dim, page, dtype, [2000, 3001, 700, 129], [600, 701, 300, 2], causal, window, g, rise=rise)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("group,rows", [(1, [1, 8, 3, 5]), (4, [1, 4, 3, 2]), (4, [8, 7, 5, 1]), (8, [4, 1, 3, 2]), (32, [1, 1, 1, 1])])
+@pytest.mark.parametrize("dim,page", [(64, 32), (128, 64), (128, 16)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 1500), (False, 0)])
+def test_attend_few_rows_of_many_tiles_a_block(dtype, group, rows, dim, page, causal, window):
+    """Some 1300 tiles for the GPU's 296 blocks, with every number of rows that has code of its own."""
+    g = torch.Generator().manual_seed(37)
+    _attend_large(8, group, dim, page, dtype, [9000, 7003, 300, 4500], rows, causal, window, g, rise=60.0 if page == 64 else 0.0)
+
+
+@gpu
+@pytest.mark.parametrize("max_q", [1, 700])
+def test_attend_mixed_batches_of_many_tiles_a_block(max_q):
+    g = torch.Generator().manual_seed(38)
+    _attend_large(4, 4, 128, 64, torch.bfloat16, [3000, 9000, 1, 4000, 2500, 5000], [700, 1, 1, 5, 300, 1], True, 0, g, max_q=max_q)
