@@ -531,7 +531,8 @@ wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows
  *   lse       [dev] f32[n_rows][q_heads] or NULL
  *   q_heads   a multiple of kv_heads, at most 64 * kv_heads; n_rows * q_heads / kv_heads <= 2^24
  *   max_q     the most rows any request has, as far as the caller knows (1: a step of single tokens).  It
- *             chooses the kernels; requests with more rows are answered all the same, more slowly
+ *             chooses the kernels; requests with more rows are answered all the same, more slowly.  0 only
+ *             where n_rows is 0: then nothing is launched
  *   options   WM_ATTEND_CAUSAL or 0
  *   workspace [dev] wm_pages_workspace_bytes(head_dim) bytes, 16-byte aligned, contents arbitrary.  One call's at a time:
  *             calls (or captured graphs) that may run side by side need one each

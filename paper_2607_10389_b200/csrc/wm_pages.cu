@@ -214,13 +214,13 @@ wm_status wm_pages_attend(const wm_pages* pages, const int32_t* table, uint32_t 
     if (!pages_ok(pages, shift) || !q || !out || !table || !kv_len || !q_start) return WM_ERR_ARG;
     if ((type != WM_TYPE_BF16 && type != WM_TYPE_F16) || (options & ~WM_ATTEND_CAUSAL) || (window && !(options & WM_ATTEND_CAUSAL))) return WM_ERR_ARG;
     if (n_requests == 0 || n_requests > kMaxRequests || table_stride == 0 || (uint64_t)n_requests * table_stride >= (1ull << 31)) return WM_ERR_ARG;
-    if ((uint64_t)table_stride << shift > (1ull << 30) || n_rows >= (1u << 24) || max_q == 0 || !std::isfinite(scale)) return WM_ERR_ARG;
+    if ((uint64_t)table_stride << shift > (1ull << 30) || n_rows >= (1u << 24) || !std::isfinite(scale)) return WM_ERR_ARG;
     if (q_heads == 0 || q_heads % pages->kv_heads || q_heads / pages->kv_heads > 64u) return WM_ERR_ARG;
     if ((uint64_t)n_rows * (q_heads / pages->kv_heads) > (1ull << 24)) return WM_ERR_ARG;
     if (!workspace || !aligned16(workspace) || workspace_bytes < wm_pages_workspace_bytes(pages->head_dim)) return WM_ERR_ARG;
     g_launches = 0;
     if (n_rows == 0) return WM_OK;
-    if (!rows_ok(q, 2) || !rows_ok(out, 2)) return WM_ERR_ARG;
+    if (!rows_ok(q, 2) || !rows_ok(out, 2) || max_q == 0) return WM_ERR_ARG;
     if ((n_rows > 1 && out->row_stride < pages->head_dim) || (q_heads > 1 && out->head_stride < pages->head_dim)) return WM_ERR_ARG;
     if (window >= (1u << 30)) window = 0;             // (no request is longer: such a window hides nothing)
     const AttendArgs a = {*pages, shift, table, table_stride, kv_len, q_start, n_requests, q->ptr, out->ptr, q->row_stride, q->head_stride,

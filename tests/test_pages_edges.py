@@ -193,3 +193,18 @@ def test_attend_few_rows_of_many_tiles_a_block(dtype, group, rows, dim, page, ca
 def test_attend_mixed_batches_of_many_tiles_a_block(max_q):
     g = torch.Generator().manual_seed(38)
     _attend_large(4, 4, 128, 64, torch.bfloat16, [3000, 9000, 1, 4000, 2500, 5000], [700, 1, 1, 5, 300, 1], True, 0, g, max_q=max_q)
+
+
+def test_attend_of_no_rows_asks_for_no_number_of_rows():
+    at, p, r = 1 << 20, tp._c_pages(), tp._c_rows()
+    assert wm.lib().wm_pages_attend(ctypes.addressof(p), at, 4, at, at, 1, r, r, 0, None, 0, 8, 0, 1.0, 1, 0, at, 1 << 30, None, None) == 0
+    assert wm.last_launch_count() == 0
+
+
+@gpu
+def test_attend_of_no_rows_with_every_number_of_rows_a_caller_may_give():
+    pages, none = wm.new_pages(4, 16, 2, 64), torch.zeros(0, 2, 64, device="cuda", dtype=torch.bfloat16)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    for kw in ({}, dict(max_q=0), dict(max_q=3)):
+        wm.wm_pages_attend(pages, i32([[0, 1]]), i32([3]), i32([0, 0]), none, none.clone(), wm.new_pages_workspace(64), **kw)
+    torch.cuda.synchronize()
