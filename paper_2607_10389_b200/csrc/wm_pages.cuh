@@ -305,6 +305,15 @@ __device__ __forceinline__ float power_not_below(float s)
     return __uint_as_float((e < 1u ? 1u : e > 254u ? 254u : e) << 23);
 }
 
+// a * b with what does not fit in 32 bits kept as an odd last bit: rounded to fewer bits afterwards, it goes where the exact
+// product would (a product rounded to nearest can come to lie on the middle of two codes).  Below the normal floats it is too small for
+// any code.
+__device__ __forceinline__ float product_to_odd(float a, float b)
+{
+    const float p = __fmul_rz(a, b);
+    return __uint_as_float(__float_as_uint(p) | (fmaf(a, b, -p) != 0.0f ? 1u : 0u));
+}
+
 // Eight elements a lane, LPR lanes a row.
 template <typename T> __device__ __forceinline__ void load8(const T* p, uint32_t (&w)[2 * sizeof(T)])
 {
@@ -439,7 +448,8 @@ k_pages_append(AppendArgs a)
                     auto four = [&](uint32_t v) {
                         const uint32_t h0 = from_e4m3x2(v), h1 = from_e4m3x2(v >> 16);
                         const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
-                        return to_e4m3x2(f0.x * ratio, f0.y * ratio) | to_e4m3x2(f1.x * ratio, f1.y * ratio) << 16;
+                        return to_e4m3x2(product_to_odd(f0.x, ratio), product_to_odd(f0.y, ratio)) |
+                               to_e4m3x2(product_to_odd(f1.x, ratio), product_to_odd(f1.y, ratio)) << 16;
                     };
                     out.x = four(in.x);
                     out.y = four(in.y);

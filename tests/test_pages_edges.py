@@ -208,3 +208,23 @@ def test_attend_of_no_rows_with_every_number_of_rows_a_caller_may_give():
     for kw in ({}, dict(max_q=0), dict(max_q=3)):
         wm.wm_pages_attend(pages, i32([[0, 1]]), i32([3]), i32([0, 0]), none, none.clone(), wm.new_pages_workspace(64), **kw)
     torch.cuda.synchronize()
+
+
+@gpu
+@pytest.mark.parametrize("code,tie", [(9.0, 8.5), (11.0, 9.5), (13.0, 12.5), (15.0, 14.5), (15.0, 7.25), (13.0, 4.5 * 2.0 ** -9)])
+def test_append_rounds_kept_codes_once(code, tie):
+    """Old scales beside those that would put a code's new value exactly between two codes: the product has more bits than a float,
+    and a float of it can lie on the middle where the product does not."""
+    page, n, new = 16, 41, 2.0
+    near = torch.tensor(tie / code, dtype=torch.float32).view(torch.int32) + torch.arange(n, dtype=torch.int32) - n // 2
+    scales = (near.view(torch.float32) * new)[:, None].contiguous()
+    k = torch.full((n, 1, page, 64), code).to(ref.E4M3).view(torch.uint8)
+    k[:, :, 1::2] = torch.tensor(-code).to(ref.E4M3).view(torch.uint8)
+    pages = wm.Pages(k.cuda(), k.cuda(), scales.cuda(), scales.cuda())
+    slots = [p * page + 5 for p in range(n)]
+    x = torch.full((n, 1, 64), 448.0 * new).cuda()
+    want = [ref.values(k), scales.double()]
+    ref.append(want[0], want[1], x.cpu(), slots, page)
+    assert (want[1] == new).all() and len(want[0][:, 0, 0, 0].unique()) == 2        # the middle is crossed
+    wm.wm_pages_append(pages, x, x, torch.tensor(slots, dtype=torch.int32, device="cuda"))
+    tp._check_pool(pages, [want[0], want[0], want[1], want[1]])
