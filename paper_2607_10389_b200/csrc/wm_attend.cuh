@@ -158,10 +158,10 @@ template <typename T>
 __device__ __forceinline__ void store_joined(const AttendArgs& a, const Request& r, uint32_t gr, uint32_t head, uint32_t d, float m, float R, float l, const float (&o)[4])
 {
     const uint32_t qrow = (uint32_t)r.start + gr / a.group, qh = head * a.group + gr % a.group;
-    const float factor = exp2_fast(R == -INFINITY ? 0.0f : R - m);
+    const float factor = exp2_to_zero(R == -INFINITY ? 0.0f : R - m);
     __align__(8) T out[4];
 #pragma unroll
-    for (int k = 0; k < 4; k++) from_float(out[k], l == 0.0f ? 0.0f : o[k] * factor / l);
+    for (int k = 0; k < 4; k++) from_float(out[k], l == 0.0f ? 0.0f : o[k] / l * factor);        // (the other way round a large or small scale leaves the floats)
     *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + (size_t)qrow * a.o_row + (size_t)qh * a.o_head + d) = *reinterpret_cast<const uint2*>(out);
     if (d == 0 && a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
@@ -697,7 +697,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                         if (dead) sum = NAN;
                         if (full) {
                             const uint32_t gr = row0 + i, qrow = (uint32_t)r.start + gr / a.group, qh = head * a.group + gr % a.group;
-                            const float v = sum == 0.0f ? 0.0f : o[k] * exp2_fast(mr.y == -INFINITY ? 0.0f : mr.y - mr.x) / sum;
+                            const float v = sum == 0.0f ? 0.0f : o[k] / sum * exp2_to_zero(mr.y == -INFINITY ? 0.0f : mr.y - mr.x);
                             if (tid < D) store_out<T>(a, qrow, qh, tid, v);
                             if (tid == 0 && a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = sum == 0.0f ? -INFINITY : (mr.x + log2f(sum)) * 0.6931471805599453f;
                         } else {

@@ -142,6 +142,13 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// The same down to the smallest floats: for the outputs' last factor.
+__device__ __forceinline__ float exp2_to_zero(float x)
+{
+    float r;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 __device__ __forceinline__ float warp_min(float x)
 {
     float r;

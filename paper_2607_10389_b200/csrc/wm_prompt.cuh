@@ -52,7 +52,7 @@ template <typename T, int D> struct Many {
 };
 
 // A weight of the reference's size is 2^kTop in f16; up to 2^kRoom more fits in (2^15 of 65504), and what is 2^-25 below is lost.
-constexpr float kTop = 1.0f, kRoom = 14.0f;
+constexpr float kTop = 1.0f, kRoom = 14.0f, kOne = 0.5f;        // kOne: 2^-kTop
 // Registers a thread: at launch (five warpgroups), then of the four softmax warpgroups and of the fifth.
 constexpr uint32_t kManyRegs = 96, kSoftmaxRegs = 104, kOtherRegs = 64;
 static_assert(4 * kSoftmaxRegs + kOtherRegs <= 5 * kManyRegs, "dealt out from what there is at launch");
@@ -696,7 +696,9 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                     m = m1;
                 }
                 const bool dead = *(volatile uint32_t*)&M.dead;
-                const float factor = dead ? NAN : !full ? 1.0f : l == 0.0f ? 0.0f : exp2_fast(R == -INFINITY ? 0.0f : R - kTop - m) / l;
+                // (two factors: their product leaves the floats where a value scale is small and l is large)
+                const float over_l = dead ? NAN : !full ? kOne : l == 0.0f ? 0.0f : kOne / l;
+                const float factor = !full || R == -INFINITY ? 1.0f : exp2_to_zero(R - m);
                 const bool nan = *(volatile uint32_t*)&M.nan_seen != 0u;
                 const int32_t row1 = (int32_t)min((s.rt + 1u) * kManyRows, n_rows) - 1;
                 const Span span = span_of(a, s.r.kv, s.r.kv - s.r.rows + (int32_t)(s.rt * kManyRows / a.group), s.r.kv - s.r.rows + row1 / (int32_t)a.group);
@@ -711,7 +713,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                     tmem_read32(tO + ch * 32u, x);
                     tmem_wait_loads();
 #pragma unroll
-                    for (int i = 0; i < 32; i++) x[i] = l == 0.0f && full && !dead ? 0.0f : x[i] * factor;
+                    for (int i = 0; i < 32; i++) x[i] = l == 0.0f && full && !dead ? 0.0f : x[i] * over_l * factor;
                     if (nan && live) {
                         // rare: NaN values among the tokens that only some rows see
 #pragma unroll 1
@@ -755,7 +757,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                         if (a.lse) a.lse[(size_t)qrow * a.q_heads + qh] = dead ? NAN : l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
                     } else {
                         *reinterpret_cast<float4*>(W.parts + (size_t)(blockIdx.x * 2u + slot) * kManyPartFloats + kManyRows * 128 + 4 * local) =
-                            make_float4(m, R - kTop, dead ? NAN : l, 0.0f);
+                            make_float4(m, R, dead ? NAN : l, 0.0f);
                     }
                 }
                 if (!full && s.j == 0 && tid == 0) {

@@ -1,5 +1,6 @@
 """The paged 8-bit cache at its edges: rows that see nothing of a tile, zeros, extreme scales, long axes, refusals."""
 import ctypes
+import math
 
 import pytest
 import torch
@@ -228,3 +229,35 @@ def test_append_rounds_kept_codes_once(code, tie):
     assert (want[1] == new).all() and len(want[0][:, 0, 0, 0].unique()) == 2        # the middle is crossed
     wm.wm_pages_append(pages, x, x, torch.tensor(slots, dtype=torch.int32, device="cuda"))
     tp._check_pool(pages, [want[0], want[0], want[1], want[1]])
+
+
+@gpu
+@pytest.mark.parametrize("rows,max_q", [([1, 1], 1), ([3, 8], 8), ([60, 140], 140), ([60, 140], 1)])
+@pytest.mark.parametrize("exponent", [119, 110, -120, -126, -130])
+def test_attend_values_at_the_ends_of_the_floats(rows, max_q, exponent):
+    """Values up to 1.75 * 2^127: their weighted sums leave 32 bits where their means do not."""
+    g = torch.Generator().manual_seed(34)
+    lens = [300, 5000]
+    pages, arrays, table = tp._attend_case(lens, 64, 2, 64, g)
+    arrays[1].fill_(0x7E), arrays[3].fill_(2.0 ** exponent)
+    pages.v.copy_(arrays[1]), pages.v_scale.copy_(arrays[3])
+    q = 0.1 * torch.randn((sum(rows), 2, 64), generator=g)
+    tp._attend(pages, arrays, table, lens, rows, 2, torch.bfloat16, g, q=q, max_q=max_q)
+
+
+@gpu
+@pytest.mark.parametrize("exponent", [119, 0, -126])
+@pytest.mark.parametrize("requests,rows,heads", [(1, 1, 1), (20, 3, 16), (1, 200, 1), (1, 2560, 16)])
+def test_attend_means_of_a_quarter_of_a_million_values_at_the_ends_of_the_floats(exponent, requests, rows, heads):
+    """Equal weights and equal values: every sum is a whole number that a float holds, and the mean is the value.  A unit in parts, and
+    whole."""
+    n, page = 1 << 18, 128
+    k, v = torch.zeros((n // page, heads, page, 64), dtype=torch.uint8, device="cuda"), torch.full((n // page, heads, page, 64), 0x7E, dtype=torch.uint8, device="cuda")
+    pages = wm.Pages(k, v, torch.ones((n // page, heads), device="cuda"), torch.full((n // page, heads), 2.0 ** exponent, device="cuda"))
+    table = torch.arange(n // page, dtype=torch.int32, device="cuda").repeat(requests, 1)
+    q = torch.zeros((requests * rows, heads, 64), dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+    wm.wm_pages_attend(pages, table, tp._dev([n] * requests), tp._dev([rows * i for i in range(requests + 1)]), q, out, wm.new_pages_workspace(64), lse=lse,
+                       causal=False, max_q=rows)
+    assert (out.float() == 448.0 * 2.0 ** exponent).all()
+    assert (lse.double() - 18 * math.log(2.0)).abs().max() <= 2.0 ** -18 + 2.0 ** -22 * 13
