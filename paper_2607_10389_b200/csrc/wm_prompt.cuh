@@ -15,9 +15,10 @@ namespace wm {
 //            (exact) by a warpgroup of its own, for all 256 rows.
 // Two threads have one row, 64 of a tile's tokens each (one thread a row left every scheduler with two warps at work, which waited for
 // their own results most of the time).  They have to agree only where O's reference moves; sums meet at the end.  As in the kernel for few rows the pages' scales act in f32,
-// the values' as an exponent; O is referred to a maximum R of weighted scores that follows only in jumps of more than 2^14
-// (weights lie in f16 from 2 on downwards, so up to 2^15 there is room), which makes rescaling O in tensor memory rare: a warp that does it
-// holds up the other three of its tile for 900 cycles, and with jumps of 2^7 one of them did in every other tile.
+// the values' as an exponent; O is referred to a maximum R of weighted scores that follows only in jumps (of more than 2^14 in units of up
+// to 16384 tokens, see top_of: weights lie in f16 from 2 on downwards, so up to 2^15 there is room), which makes rescaling O in tensor
+// memory rare: a warp that does it holds up the other three of its tile for 900 cycles, and with jumps of 2^7 one of them did in every
+// other tile.
 // Work is dealt out as in the kernel for few rows: equal shares of tiles, units cut between workers are joined in order.
 //
 // Measured: four prompts' 1024 rows over 5000 to 9000 tokens (32 heads, 8 key heads of 128; 437 GFLOP) 393 us, 1.11 PFLOP/s, 0.68 of the
@@ -51,8 +52,14 @@ template <typename T, int D> struct Many {
     static constexpr uint32_t kSmem = oMisc + (uint32_t)sizeof(Misc) + 1024;
 };
 
-// A weight of the reference's size is 2^kTop in f16; up to 2^kRoom more fits in (2^15 of 65504), and what is 2^-25 below is lost.
-constexpr float kTop = 1.0f, kRoom = 14.0f, kOne = 0.5f;        // kOne: 2^-kTop
+// Weights lie in f16 up to 2^kRoom (of 65504); one of the size that the reference is set to is 2^top.  What is below 2^-25 is lost from
+// the outputs, though not from l: so that even N tokens that far below the largest weight miss no more than 2^-12 of it in all (as much
+// as the weights' 11 bits may), top grows with the unit's tokens, from 1 up to 2^14 of them to 12 from 2^25 on.  Small where it can be,
+// for the reference's jumps: measured (us), four prompts' 1024 rows over 5000 to 9000 tokens 448 with 1, 466 with 4, 495 with 6, 543 with
+// 7; 1360 rows on 6800 tokens 117, 137, 165, 181.  In a long unit the jumps are few among its tiles: 1024 rows on 131072 tokens 2100 with
+// 1, 2230 with the 5 they get.
+constexpr float kRoom = 15.0f;
+__device__ __forceinline__ int32_t top_of(uint32_t tiles) { return min(max(32 - __clz((int)(tiles - 1u)) - 6, 1), 12); }
 // Registers a thread: at launch (five warpgroups), then of the four softmax warpgroups and of the fifth.
 constexpr uint32_t kManyRegs = 96, kSoftmaxRegs = 104, kOtherRegs = 64;
 static_assert(4 * kSoftmaxRegs + kOtherRegs <= 5 * kManyRegs, "dealt out from what there is at launch");
@@ -494,8 +501,9 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                     if (half == 0u && line == 0u) M.seg[w] = s;       // (read again when the unit's part ends: in registers it would cost the loop)
                 }
                 const float f = live && lo < hi ? M.f[local] : 1.0f;      // (a row that sees nothing: whatever its query is)
-                float m = -INFINITY, l = 0.0f, R = -INFINITY;       // R: what O refers to
+                float m = -INFINITY, l = 0.0f, R = -INFINITY;       // R: what O refers to, less `top`
                 const uint32_t count = s.count;
+                const float top = (float)top_of(s.nt);
                 for (uint32_t c = 0; c < count; c++, t0 += 128) {
                     auto written = [&](uint32_t part) {
                         tmem_wait_stores();
@@ -552,7 +560,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                         if (c == 0) {
                             M.other[w][half][line].x = rt;
                             both();
-                            R = fmaxf(rt, M.other[w][half ^ 1u][line].x);
+                            R = fmaxf(rt, M.other[w][half ^ 1u][line].x) - top;
                         }
                         const float Rb = R == -INFINITY ? 0.0f : R, mb = mt == -INFINITY ? Rb : mt;
                         // all 256 threads of the tile have to say so before the weights are handed on; they are asked here and heard when the first
@@ -572,7 +580,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                                     if (at % GS == 0) {
                                         const float2 z = scale(at / GS);
                                         fac2.x = fac2.y = z.x * f;
-                                        off2.x = off2.y = z.y - Rb + kTop;
+                                        off2.x = off2.y = z.y - Rb;
                                     }
                                     float2 e = fma2(make_float2(x[at], x[at + 1]), fac2, off2);
                                     e.x = exp2_fast(e.x);
@@ -630,7 +638,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                         if (c == 0) R = -INFINITY;
                         const bool jump = rt > R + kRoom;
                         if (__any_sync(0xFFFFFFFFu, jump)) {
-                            const float R1 = jump ? rt : R;
+                            const float R1 = jump ? rt - top : R;
                             const float factor = R == -INFINITY ? 0.0f : exp2_fast(R - R1);
                             R = R1;
                             if (c > 0) {                                             // (either thread of a row has half of its channels)
@@ -665,12 +673,12 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                             }
 #pragma unroll
                             for (int i = 0; i < 32; i += 2) {
-                                const float off = (i < 16 ? lv0 : lv1) - Rb + kTop;
+                                const float off = (i < 16 ? lv0 : lv1) - Rb;
                                 const float y0 = exp2_fast(v[i] + off), y1 = exp2_fast(v[i + 1] + off);
                                 sum[i / 16] += y0 + y1;
                                 pk[i / 2] = pack_half2(y0, y1);
                             }
-                            if (!apart) l += sum[0] * exp2_fast(Rb - kTop - lv0 - mb) + sum[1] * exp2_fast(Rb - kTop - lv1 - mb);
+                            if (!apart) l += sum[0] * exp2_fast(Rb - lv0 - mb) + sum[1] * exp2_fast(Rb - lv1 - mb);
                             tmem_write16(tS + ch * 16u, pk);
                         }
                         written(0);
@@ -697,7 +705,9 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                 }
                 const bool dead = *(volatile uint32_t*)&M.dead;
                 // (two factors: their product leaves the floats where a value scale is small and l is large)
-                const float over_l = dead ? NAN : !full ? kOne : l == 0.0f ? 0.0f : kOne / l;
+                const float one = __uint_as_float((uint32_t)(127 - top_of(s.nt)) << 23);
+                R += (float)top_of(s.nt);
+                const float over_l = dead ? NAN : !full ? one : l == 0.0f ? 0.0f : one / l;
                 const float factor = !full || R == -INFINITY ? 1.0f : exp2_to_zero(R - m);
                 const bool nan = *(volatile uint32_t*)&M.nan_seen != 0u;
                 const int32_t row1 = (int32_t)min((s.rt + 1u) * kManyRows, n_rows) - 1;

@@ -261,3 +261,37 @@ def test_attend_means_of_a_quarter_of_a_million_values_at_the_ends_of_the_floats
                        causal=False, max_q=rows)
     assert (out.float() == 448.0 * 2.0 ** exponent).all()
     assert (lse.double() - 18 * math.log(2.0)).abs().max() <= 2.0 ** -18 + 2.0 ** -22 * 13
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("rows,heads,dim", [(2560, 16, 64), (64, 1, 128), (8, 16, 64)])
+@pytest.mark.parametrize("bits", [20, 27])
+def test_attend_one_token_far_above_half_a_million_others(dtype, rows, heads, dim, bits):
+    """The first token weighs 2^bits times as much as each of the others, which together still count: 1 / 256 of it where bits is 27.
+    In one unit from end to end, and in parts."""
+    n, page = 1 << 19, 128
+    k = torch.zeros((2, heads, page, dim), dtype=torch.uint8)
+    v = torch.full_like(k, 0x38)                         # ones
+    k[0, :, 0] = 0x38
+    v[0, :, 0, ::2] = 0                                  # half of the channels have nothing of the first token
+    ones = torch.ones((2, heads), device="cuda")
+    pages = wm.Pages(k.cuda(), v.cuda(), ones, ones.clone())
+    table = torch.ones((1, n // page), dtype=torch.int32, device="cuda")
+    table[0, 0] = 0
+    q = torch.ones((rows, heads, dim), dtype=dtype, device="cuda")
+    out, lse = torch.zeros_like(q), torch.zeros((rows, heads), device="cuda")
+    score = bits * math.log(2.0)
+    wm.wm_pages_attend(pages, table, tp._dev([n]), tp._dev([0, rows]), q, out, wm.new_pages_workspace(dim), lse=lse, scale=score / dim,
+                       causal=False, max_q=rows)
+    others = (n - 1) * 2.0 ** -bits
+    want = torch.ones(dim, dtype=torch.float64, device="cuda")
+    want[::2] = others / (1.0 + others)
+    # products and sums of ones are exact; the score has a handful of factors, each rounded by 2^-24 of it; weights have 11 bits, and what
+    # is below their grid is no more than 2^-12 of the largest in all.  The tensor cores lose what is below 2^-25 of the sum that it
+    # is added to: nothing where that holds nothing of the first token
+    d = 8 * 2.0 ** -24 * score
+    far = want * (2.0 ** -12 + 2 * d + torch.finfo(dtype).eps / 2 + n * 2.0 ** -25) + 2.0 ** -12
+    off = (out.double() - want).abs()
+    assert (off <= far).all(), (off / far).max()
+    assert ((lse.double() - score - math.log1p(others)).abs() <= d + 2.0 ** -18 + 2.0 ** -22 * score).all()
