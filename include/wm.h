@@ -428,6 +428,7 @@ wm_status wm_checksum_noalloc(const void* cache, uint64_t nbytes, uint32_t chunk
  *
  * A pool has n_pages pages of page_tokens tokens.  Keys and values are e4m3 codes; one f32 scale
  * for every page and head (for keys and for values) gives value = code * scale.
+ * What the calls take as 32-bit words (lists, tables, scales, lse, reports) is 4-byte aligned; other addresses are refused.
  */
 typedef struct {
     void*    k;             /* [dev] e4m3 codes; token t, head h, page p, channel d at k + p * page_stride + h * head_stride + t * token_stride + d */

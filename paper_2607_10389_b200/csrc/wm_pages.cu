@@ -6,6 +6,7 @@
 #include <cstdint>
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <mutex>
 #include <type_traits>
 
@@ -23,11 +24,19 @@
 
 namespace wm {
 
+// Whether words may be read and written at all of these (NULL included).
+static bool words_ok(std::initializer_list<const void*> at)
+{
+    for (const void* p : at)
+        if ((reinterpret_cast<uintptr_t>(p) & 3u) != 0) return false;
+    return true;
+}
+
 // The pool's geometry: what every call checks before anything is launched.
 static bool pages_ok(const wm_pages* p, uint32_t& shift)
 {
     if (!p || !p->k || !p->v || !p->k_scale || !p->v_scale) return false;
-    if (!aligned16(p->k) || !aligned16(p->v)) return false;
+    if (!aligned16(p->k) || !aligned16(p->v) || !words_ok({p->k_scale, p->v_scale})) return false;
     if (((p->page_stride | p->head_stride | p->token_stride) & 15u) != 0) return false;
     shift = p->page_tokens == 16 ? 4 : p->page_tokens == 32 ? 5 : p->page_tokens == 64 ? 6 : p->page_tokens == 128 ? 7 : 0;
     if (!shift || (p->head_dim != 64 && p->head_dim != 128)) return false;
@@ -165,6 +174,7 @@ wm_status wm_pages_plan(const int32_t* old_len, const int32_t* new_len, uint32_t
 {
     const uint32_t shift = page_tokens == 16 ? 4 : page_tokens == 32 ? 5 : page_tokens == 64 ? 6 : page_tokens == 128 ? 7 : 0;
     if (!old_len || !new_len || !table || !free_pages || !free_count || !free_count_out || !start || (!slots && n_slots)) return WM_ERR_ARG;
+    if (!words_ok({old_len, new_len, table, free_pages, free_count, free_count_out, start, slots, report})) return WM_ERR_ARG;
     if (!shift || n_requests == 0 || n_requests > kMaxRequests || table_stride == 0 || n_slots >= (1u << 31)) return WM_ERR_ARG;
     if (n_pages == 0 || ((uint64_t)n_pages << shift) >= (1ull << 31) || (uint64_t)n_requests * table_stride >= (1ull << 31)) return WM_ERR_ARG;
     const PlanArgs a = {old_len, new_len, n_requests, page_tokens, shift, n_pages, table, table_stride, free_pages, free_count,
@@ -187,7 +197,7 @@ wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows
     uint32_t shift = 0;
     if (type < WM_TYPE_BF16 || type > WM_TYPE_F32) return WM_ERR_ARG;
     const uint32_t size = type == WM_TYPE_F32 ? 4 : 2;
-    if (!pages_ok(pages, shift) || !k || !v || n_rows >= (1u << 24)) return WM_ERR_ARG;
+    if (!pages_ok(pages, shift) || !k || !v || n_rows >= (1u << 24) || !words_ok({slots, report})) return WM_ERR_ARG;
     g_launches = 0;
     if (n_rows == 0) return WM_OK;
     if (!rows_ok(k, size) || !rows_ok(v, size) || !slots) return WM_ERR_ARG;
@@ -212,6 +222,7 @@ wm_status wm_pages_attend(const wm_pages* pages, const int32_t* table, uint32_t 
 {
     uint32_t shift = 0;
     if (!pages_ok(pages, shift) || !q || !out || !table || !kv_len || !q_start) return WM_ERR_ARG;
+    if (!words_ok({table, kv_len, q_start, lse, report})) return WM_ERR_ARG;
     if ((type != WM_TYPE_BF16 && type != WM_TYPE_F16) || (options & ~WM_ATTEND_CAUSAL) || (window && !(options & WM_ATTEND_CAUSAL))) return WM_ERR_ARG;
     if (n_requests == 0 || n_requests > kMaxRequests || table_stride == 0 || (uint64_t)n_requests * table_stride >= (1ull << 31)) return WM_ERR_ARG;
     if ((uint64_t)table_stride << shift > (1ull << 30) || n_rows >= (1u << 24) || !std::isfinite(scale)) return WM_ERR_ARG;

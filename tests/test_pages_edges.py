@@ -295,3 +295,28 @@ def test_attend_one_token_far_above_half_a_million_others(dtype, rows, heads, di
     off = (out.double() - want).abs()
     assert (off <= far).all(), (off / far).max()
     assert ((lse.double() - score - math.log1p(others)).abs() <= d + 2.0 ** -18 + 2.0 ** -22 * score).all()
+
+
+def _plan_args(**change):
+    f = {n: 1 << 20 for n in ("old", "new", "table", "free", "count", "count_out", "start", "slots", "report")}
+    f.update(change)
+    return (f["old"], f["new"], 1, 64, 10, f["table"], 4, f["free"], f["count"], f["count_out"], f["start"], f["slots"], 5, f["report"], None)
+
+
+# (only what is refused: these addresses are not looked at)
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_words_at_odd_addresses_are_refused(off):
+    """A slice of a byte tensor can be anywhere; read as words there it would end the context."""
+    lib, at, r = wm.lib(), 1 << 20, tp._c_rows()
+    for name in ("old", "new", "table", "free", "count", "count_out", "start", "slots", "report"):
+        assert lib.wm_pages_plan(*_plan_args(**{name: at + off})) == -1, name
+    for change in (dict(k_scale=at + off), dict(v_scale=at + off)):
+        p = tp._c_pages(**change)
+        assert lib.wm_pages_append(ctypes.addressof(p), r, r, 0, at, 1, None, None) == -1, change
+        assert lib.wm_pages_attend(ctypes.addressof(p), at, 4, at, at, 1, r, r, 0, None, 1, 8, 1, 1.0, 1, 0, at, 1 << 30, None, None) == -1, change
+    p = tp._c_pages()
+    for slots, report in ((at + off, at), (at, at + off)):
+        assert lib.wm_pages_append(ctypes.addressof(p), r, r, 0, slots, 1, report, None) == -1
+    for i in range(5):
+        a = [at + off * (i == j) for j in range(5)]
+        assert lib.wm_pages_attend(ctypes.addressof(p), a[0], 4, a[1], a[2], 1, r, r, 0, a[3], 1, 8, 1, 1.0, 1, 0, at, 1 << 30, a[4], None) == -1, i
