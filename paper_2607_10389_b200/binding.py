@@ -417,6 +417,7 @@ _TYPES = {torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16, torch.float32: TYP
 ATTEND_CAUSAL = 1
 PAGES_MAX_REQUESTS = 4000
 PAGES_REPORT_BYTES = 16
+_WORD = 1 << 32                                  # what ctypes would cut numbers to without a word
 
 
 class Pages:
@@ -535,6 +536,8 @@ def wm_pages_plan(old_len: torch.Tensor, new_len: torch.Tensor, page_tokens: int
     """Block tables, free list, row offsets and slot map of a step (see include/wm.h).  All tensors are int32;
     `free_count_out` may be `free_count`."""
     here, n = _here(), old_len.numel()
+    if not 0 < page_tokens < _WORD:
+        raise WmError("page_tokens must be 16, 32, 64 or 128")
     tab, width = _table(table, n, here)
     n_slots = slots.numel()
     rc = lib().wm_pages_plan(_i32(old_len, None, "old_len", here), _i32(new_len, n, "new_len", here), n, page_tokens, free_pages.numel(),
@@ -567,6 +570,7 @@ def wm_pages_attend(pages: Pages, table: torch.Tensor, kv_len: torch.Tensor, q_s
         raise WmError("q must be (rows, heads, channels) and out have its type and shape")
     if window < 0 or (max_q is not None and max_q < 0):
         raise WmError("window and max_q must not be negative")
+    window = min(window, _WORD - 1)            # (far beyond every request already)
     rows, heads, _ = shape
     if lse is not None and not (lse.dtype is torch.float32 and lse.get_device() == here and lse.shape == (rows, heads) and lse.is_contiguous()):
         _refuse(lse, "lse", here)
@@ -577,7 +581,7 @@ def wm_pages_attend(pages: Pages, table: torch.Tensor, kv_len: torch.Tensor, q_s
     tab, width = _table(table, n, here)
     rc = lib().wm_pages_attend(pages.handle(here), tab, width, _i32(kv_len, None, "kv_len", here), _i32(q_start, n + 1, "q_start", here), n,
                                _rows(q, heads, dim, "q", here), _rows(out, heads, dim, "out", here), _TYPES[q.dtype],
-                               None if lse is None else lse.data_ptr(), rows, heads, rows if max_q is None else max_q,
+                               None if lse is None else lse.data_ptr(), rows, heads, rows if max_q is None else min(max_q, _WORD - 1),
                                dim ** -0.5 if scale is None else scale, ATTEND_CAUSAL if causal else 0, window, workspace.data_ptr(),
                                workspace.numel() * workspace.element_size(), _report(report, here), _stream(stream))
     if rc:

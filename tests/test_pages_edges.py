@@ -320,3 +320,19 @@ def test_words_at_odd_addresses_are_refused(off):
     for i in range(5):
         a = [at + off * (i == j) for j in range(5)]
         assert lib.wm_pages_attend(ctypes.addressof(p), a[0], 4, a[1], a[2], 1, r, r, 0, a[3], 1, 8, 1, 1.0, 1, 0, at, 1 << 30, a[4], None) == -1, i
+
+
+@gpu
+def test_numbers_beyond_32_bits_are_not_cut():
+    g = torch.Generator().manual_seed(40)
+    lens, rows = [70, 200], [3, 150]
+    pages, arrays, table = tp._attend_case(lens, 32, 1, 64, g)
+    for window in (2 ** 32, 2 ** 32 + 5, 2 ** 40 + 1):
+        for max_q in (2 ** 32, 2 ** 32 + 1):
+            tp._attend(pages, arrays, table, lens, rows, 2, torch.bfloat16, g, window=window, max_q=max_q)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    count, start, slots, tab = i32([4]), i32([0, 0]), i32([-9] * 5), i32([[-1, -1]])
+    for page in (2 ** 32 + 16, -16, 0):
+        with pytest.raises(wm.WmError):
+            wm.wm_pages_plan(i32([0]), i32([5]), page, tab, i32([0, 1, 2, 3]), count, count, start, slots)
+    assert count.item() == 4 and slots.tolist() == [-9] * 5 and tab.tolist() == [[-1, -1]]
