@@ -121,12 +121,6 @@ struct UnitShape {
     uint32_t row_tiles, j0, nt;
     unsigned long long tiles;
 };
-// Worker w's first tile (the division in 32 bits where they hold it: the long one is a hundred instructions to wait for).
-__device__ __forceinline__ unsigned long long share_of(uint32_t w, unsigned long long total, unsigned long long workers)
-{
-    if (w >= workers) return total;
-    return total < (1u << 23) ? (unsigned long long)(w * (uint32_t)total / (uint32_t)workers) : w * total / workers;
-}
 template <int RT> __device__ __forceinline__ UnitShape shape_of(const AttendArgs& a, const Request& r)
 {
     UnitShape u;
@@ -135,7 +129,7 @@ template <int RT> __device__ __forceinline__ UnitShape shape_of(const AttendArgs
     u.j0 = (uint32_t)lo / 128u;
     const uint32_t end = ((uint32_t)r.kv + 127u) / 128u;
     u.nt = end > u.j0 ? end - u.j0 : 1u;
-    u.tiles = (unsigned long long)a.p.kv_heads * u.row_tiles * u.nt;
+    u.tiles = tiles_of(a.p.kv_heads * u.row_tiles, u.nt);
     return u;
 }
 
@@ -300,7 +294,8 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
             uint32_t stage = 0, phase = 0;
             while (t < t_end) {
                 to_request();
-                const uint32_t off = (uint32_t)(t - prefix), unit = off / u.nt, j = off - unit * u.nt, head = unit / u.row_tiles;
+                const TileAt at = tile_at(t - prefix, u.nt);
+                const uint32_t j = at.j, head = at.unit / u.row_tiles;
                 const uint32_t count = (uint32_t)min((unsigned long long)(u.nt - j), t_end - t);
                 const int32_t* row = a.table + (size_t)req * a.table_stride;
                 const uint32_t first0 = (u.j0 + j) * 128u;
@@ -355,7 +350,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
             };
             while (t < t_end) {
                 to_request();
-                const uint32_t j = (uint32_t)(t - prefix) % u.nt, count = warp_uniform((uint32_t)min((unsigned long long)(u.nt - j), t_end - t));
+                const uint32_t j = tile_at(t - prefix, u.nt).j, count = warp_uniform((uint32_t)min((unsigned long long)(u.nt - j), t_end - t));
                 mbar_wait_hot(bar(M.kfull[stage]), phase, a.wait_ns, &M.dead);
                 mbar_wait_hot(bar(M.qbar), qphase, a.wait_ns, &M.dead);
                 qphase ^= 1u;
@@ -398,7 +393,8 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
             const uint32_t qs = base_s + F::oQ, ps = base_s + F::oP;
             while (t < t_end) {
                 to_request();
-                const uint32_t off = (uint32_t)(t - prefix), unit = off / u.nt, j = off - unit * u.nt, head = unit / u.row_tiles, rt = unit % u.row_tiles;
+                const TileAt at = tile_at(t - prefix, u.nt);
+                const uint32_t j = at.j, head = at.unit / u.row_tiles, rt = at.unit % u.row_tiles;
                 const uint32_t count = (uint32_t)min((unsigned long long)(u.nt - j), t_end - t);
                 const uint32_t row0 = rt * RT, rows = min((uint32_t)RT, (uint32_t)r.rows * a.group - row0);
                 // what the unit's first and last row see: [lo, hi)
@@ -709,7 +705,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
                 if (!full && j == 0 && tid == 0) {
                     // the worker that has the unit's last tile
                     const unsigned long long last = t + u.nt - 1;
-                    Cut cut = {1u, req, head, rt, (uint32_t)(((last + 1) * workers - 1) / total), slot, {0, 0}};
+                    Cut cut = {1u, req, head, rt, worker_of(last, total, workers), slot, {0, 0}};
                     reinterpret_cast<Cut*>(a.ws)[blockIdx.x] = cut;
                 }
                 asm volatile("bar.sync 1, 128;" ::: "memory");

@@ -17,6 +17,7 @@
 #include "wm_device.cuh"
 #include "wm_host.h"
 #include "wm_launch.h"
+#include "wm_units.h"
 #include "wm_pages.cuh"
 #include "wm_mma.cuh"
 #include "wm_attend.cuh"

@@ -154,12 +154,13 @@ k_attend_groups(AttendArgs a)
     unsigned long long base = 0;
     for (uint32_t g0 = 0; g0 < groups; g0 += 1024) {
         const uint32_t g = g0 + tid;
-        uint32_t req = 0, rt = 0, tiles = 0;
+        uint32_t req = 0, rt = 0;
+        unsigned long long tiles = 0;
         if (g < groups) {
             req = last_not_above(s_first, a.n, g);
             rt = g - s_first[req];
             uint32_t j0;
-            tiles = group_tiles(a, request_of(a, req), rt, j0) * a.p.kv_heads;
+            tiles = tiles_of(a.p.kv_heads, group_tiles(a, request_of(a, req), rt, j0));
         }
         unsigned long long sum;
         const unsigned long long before = scan(tiles, sum);
@@ -238,11 +239,11 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
             s.r = request_of(a, G.req);
             s.nt = group_tiles(a, s.r, G.rt, s.j0);
             s.base = G.base;
-            s.end = G.base + (unsigned long long)s.nt * a.p.kv_heads;
+            s.end = G.base + tiles_of(a.p.kv_heads, s.nt);
         }
-        const uint32_t off = (uint32_t)(t - s.base);
-        s.head = off / s.nt;
-        s.j = off - s.head * s.nt;
+        const TileAt at = tile_at(t - s.base, s.nt);
+        s.head = at.unit;
+        s.j = at.j;
         s.count = (uint32_t)min((unsigned long long)(s.nt - s.j), t_end - t);
     };
     if (t_begin < t_end) {
@@ -772,7 +773,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                 }
                 if (!full && s.j == 0 && tid == 0) {
                     const unsigned long long last = t + s.nt - 1;
-                    Cut cut = {1u, s.req, s.head, s.rt, (uint32_t)(((last + 1) * workers - 1) / total), slot, {0, 0}};
+                    Cut cut = {1u, s.req, s.head, s.rt, worker_of(last, total, workers), slot, {0, 0}};
                     W.cuts[blockIdx.x] = cut;
                 }
                 both();          // (both halves have read what the other left, and the outputs' way is free)
