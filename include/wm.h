@@ -543,7 +543,7 @@ wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows
  *             wm_wait_budget_ms); outputs that are not there are NaN
  * Sums and softmax statistics are held in 32 bits.  The result of a row does not depend on the other requests' contents.
  * Queries are held as sums of 8-bit codes: exact for elements above 2^-13 of their row's and head's largest, else off by 2^-21 of
- * that at most.  Weights have 11 bits or more; those far below the row's largest lie on a grid on which an output misses no
+ * that at most (of 2^-119 where that is larger).  Weights have 11 bits or more; those far below the row's largest lie on a grid on which an output misses no
  * more than 2^-12 of the largest weight's share times the largest value, up to 2^25 tokens.  Outputs are summed by the tensor cores,
  * which lose products below 2^-25 of the sum that they are added to.
  */

@@ -194,6 +194,10 @@ __device__ __forceinline__ void ask_scales(const AttendArgs& a, PageOf& p, uint3
     }
 }
 
+// The exponent that a query row is scaled by, of its largest element's bits: down to 2^-119, so that both powers of two that
+// come from it, 2^(7 - e) and 2^(e - 7), are floats.  A row of zeros takes any factor.
+__device__ __forceinline__ int row_exponent(uint32_t top) { return top == 0u ? 7 : min(max((int)(top >> 23) - 127, -119), 127); }
+
 template <typename T> __device__ __forceinline__ void store_out(const AttendArgs& a, uint32_t row, uint32_t qh, uint32_t d, float v)
 {
     T r;
@@ -421,7 +425,7 @@ k_attend_few(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gri
 #pragma unroll
                     for (uint32_t d = 1; d < TPR; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
                     // a power of two that brings the row's largest element to 128 .. 256 (NaN where the row is not finite)
-                    const int e = min(max((int)(top >> 23) - 127, -100), 127);
+                    const int e = row_exponent(top);
                     const float up = top >= 0x7F800000u ? NAN : __uint_as_float((uint32_t)(127 + 7 - e) << 23);
                     const float down = __uint_as_float((uint32_t)(127 - 7 + e) << 23);
                     if (part == 0) M.f[rr] = a.scale * 1.4426950408889634f * (top >= 0x7F800000u ? NAN : down);

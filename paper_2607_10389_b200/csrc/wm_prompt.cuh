@@ -472,7 +472,7 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
 #pragma unroll
                             for (uint32_t d = 1; d < LPR; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
                             // a power of two that brings the row's largest element to 128 .. 256; NaN where the row is not finite
-                            const int e = min(max((int)(top >> 23) - 127, -100), 127);
+                            const int e = row_exponent(top);
                             const bool fine = top < 0x7F800000u;
                             float up = __uint_as_float((uint32_t)(127 + 7 - e) << 23);
                             if (a.scale < 0.0f) up = -up;

@@ -336,3 +336,19 @@ def test_numbers_beyond_32_bits_are_not_cut():
         with pytest.raises(wm.WmError):
             wm.wm_pages_plan(i32([0]), i32([5]), page, tab, i32([0, 1, 2, 3]), count, count, start, slots)
     assert count.item() == 4 and slots.tolist() == [-9] * 5 and tab.tolist() == [[-1, -1]]
+
+
+@gpu
+@pytest.mark.parametrize("rows", [[1, 1], [4, 2], [200, 131]])
+@pytest.mark.parametrize("exponent", [-100, -108, -116, -120, 100, 120])
+def test_attend_queries_of_every_size(rows, exponent):
+    """Queries at the ends of bf16, over keys at the other end."""
+    g = torch.Generator().manual_seed(41)
+    lens = [300, 131]
+    pages, arrays, table = tp._attend_case(lens, 64, 2, 64, g)
+    arrays[2].fill_(2.0 ** (-6 - exponent) if exponent < 0 else 2.0 ** -126)
+    pages.k_scale.copy_(arrays[2])
+    q = torch.randn((sum(rows), 4, 64), generator=g) * 2.0 ** exponent
+    if -113 <= exponent < 0:                             # (rows whose largest element is below 2^-119 are on a coarser grid)
+        q[0] *= 2.0 ** -6
+    tp._attend(pages, arrays, table, lens, rows, 4, torch.bfloat16, g, q=q)
