@@ -523,7 +523,8 @@ wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows
  * kv_len[i] - n + j.  Query head h reads key head h / (q_heads / kv_heads).  A row at position p sees the request's tokens
  * t < kv_len[i], with causal only t <= p, with a window of w > 0 (causal only) only t > p - w.
  *   out = sum_t softmax_t(scale * q . key_t) value_t,   lse = log sum_t exp(scale * q . key_t)
- * A row that sees nothing (a position below zero, no tokens) gets zeros and -infinity.  Rows behind the last request's are
+ * A row that sees nothing (no tokens, or with causal a position below zero; without causal a row at such a position sees all tokens
+ * as any other) gets zeros and -infinity.  Rows behind the last request's are
  * left as they are.  Codes a row does not see do not touch it, whatever they hold (NaN included).
  *   table     [dev] i32[n_requests][table_stride], table_stride * page_tokens <= 2^30; kv_len [dev] i32[n_requests];
  *             q_start [dev] i32[n_requests + 1]

@@ -565,8 +565,9 @@ k_attend_many(AttendArgs a, const __grid_constant__ CUtensorMap kmap, const __gr
                         }
                         const float Rb = R == -INFINITY ? 0.0f : R, mb = mt == -INFINITY ? Rb : mt;
                         // all 256 threads of the tile have to say so before the weights are handed on; they are asked here and heard when the first
-                        // weights are done (waited for at once, their answer took 290 cycles)
-                        if (odd || rt > R + kRoom || !(Rb - least - mb <= 80.0f)) M.again[w][sp] = 1u;
+                        // weights are done (waited for at once, their answer took 290 cycles).  Rows that are not there are not asked: they may
+                        // be looking at what is behind the last page, which is whatever the stage held before
+                        if (live && (odd || rt > R + kRoom || !(Rb - least - mb <= 80.0f))) M.again[w][sp] = 1u;
                         mbar_arrive_at(bar(M.votes[w]));
                         {
                             float sum_l = 0.0f;

@@ -352,3 +352,30 @@ def test_attend_queries_of_every_size(rows, exponent):
     if -113 <= exponent < 0:                             # (rows whose largest element is below 2^-119 are on a coarser grid)
         q[0] *= 2.0 ** -6
     tp._attend(pages, arrays, table, lens, rows, 4, torch.bfloat16, g, q=q)
+
+
+@gpu
+@pytest.mark.parametrize("page", [16, 32])
+@pytest.mark.parametrize("lens,rows", [([90], [60]), ([90, 220, 35, 350] * 4, [60, 50, 40, 200] * 4)])
+def test_attend_gives_the_same_bits_whatever_was_in_shared_memory(page, lens, rows):
+    """Rows that fill a tile up see what a call before has left behind the last page: they have no say in how the others are computed."""
+    g = torch.Generator().manual_seed(42)
+    pages, arrays, table = tp._attend_case(lens, page, 8, 128, g)
+    pages.v_scale.fill_(2.0 ** -90)
+    before, one = wm.new_pages(1, 128, 16, 128), tp._dev([[0] * 8])
+    starts = [0]
+    for r in rows:
+        starts.append(starts[-1] + r)
+    q = torch.randn((starts[-1], 8, 128), generator=g).to(torch.bfloat16).cuda()
+    qb, ob, ws = torch.zeros((600, 16, 128), device="cuda", dtype=torch.bfloat16), torch.zeros((600, 16, 128), device="cuda", dtype=torch.bfloat16), wm.new_pages_workspace(128)
+    many, at = (tp._dev([1024]), tp._dev([0, 600])), (tp._dev(table), tp._dev(lens), tp._dev(starts))
+    got = []
+    for code in (0x7F, 0x00, 0x7F, 0x38):
+        out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+        before.k.fill_(code), before.v.fill_(code)
+        torch.cuda.synchronize()
+        wm.wm_pages_attend(before, one, *many, qb, ob, ws, causal=False, max_q=600)
+        wm.wm_pages_attend(pages, *at, q, out, ws, lse=lse, causal=False, max_q=max(rows))
+        got.append((out.cpu(), lse.cpu()))
+    for out, lse in got[1:]:
+        assert torch.equal(out, got[0][0]) and torch.equal(lse, got[0][1])
