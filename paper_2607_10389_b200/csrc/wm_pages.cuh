@@ -440,7 +440,7 @@ k_pages_append(AppendArgs a)
             scale = fmaxf(scale, power_not_below(old));
             if (scale != old) {
                 const float ratio = __fdiv_rn(old, scale);
-#pragma unroll 4
+#pragma unroll 2
                 for (uint32_t t = sub; t < off; t += RPL) {
                     uint2* c = reinterpret_cast<uint2*>(codes + (size_t)t * a.p.token_stride);
                     const uint2 in = *c;
