@@ -60,7 +60,8 @@ __device__ __forceinline__ Request few_request_of(const AttendArgs& a, uint32_t 
 //   outputs  O[channel][column] = sum_token V[token][channel] P[token][column]   (V as it lies: MN-major)
 // Both are e4m3 x e4m3 with f32 sums.  Queries and weights have more than e4m3's four bits, so each is held as a sum of pieces
 // in columns of their own, every piece the rounded remainder of the one before times 16: 4 bits a piece, two for a bf16 query
-// (8 bits: exact for elements above 2^-18 of the row's largest), three for f16's 11 bits and for the weights.  The columns are
+// (8 bits: exact for elements above 2^-13 of the row's largest, else off by 2^-21 of it at most), three for f16's 11 bits and for the
+// weights.  The columns are
 // there anyway: an MMA of 128 rows costs as much for 16 columns as for 8.
 // A page's scales are applied in f32: the key's to the score, the value's to the weight (as an addition of its logarithm in the
 // exponent, so that weights keep their bits however far apart the scales are): p' = 2^(x + log2 vs - R) <= 1 with a running
@@ -71,7 +72,8 @@ __device__ __forceinline__ Request few_request_of(const AttendArgs& a, uint32_t 
 // leaves (o, m, R, l) in the workspace, and k_attend_join puts the pieces together in the workers' order (no atomics: the
 // result does not depend on timing).
 //
-// Measured: 64 single rows over 705 MB of codes (8 key heads of 128, groups of 8) 122 us, 5.8 TB/s, 0.89 of the copy rate; one row over
+// Measured: 64 single rows over 705 MB of codes (8 key heads of 128, groups of 8) 123 us, 5.7 TB/s, 0.88 of the copy rate in short
+// runs, 131 us, 0.83, in runs of seconds; one row over
 // 2 MB 9.5 us, of which 5 are the first tile's way (4000 cycles until a block knows its share, the copy, one tile's chain).
 
 template <typename T, int D, int RT> struct Few {

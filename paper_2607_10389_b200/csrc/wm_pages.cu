@@ -54,10 +54,12 @@ static bool rows_ok(const wm_rows* r, uint32_t size)
     return r && r->ptr && aligned16(r->ptr) && (r->row_stride * size) % 16 == 0 && (r->head_stride * size) % 16 == 0;
 }
 
-constexpr uint64_t kAppendWarps = 148 * 64;
-// Rows a warp looks at: one while that many warps still fit the GPU a few times over, up to 32 beyond.  Measured, 17,000 rows of
-// prompts in pages of 64, 8 key heads of 128: 20 us with up to 32 rows a warp, 22 with 16; with one (and more work a row), 73.  Loads of 16
-// bytes a lane that stay in registers: 8 there (20 us; 4: 21.4, 16: 20.5), 4 where a warp looks at one row (256 rows: 3.5 us, with 16 7.7).
+constexpr uint64_t kAppendWarps = 148 * 64;             // (of a whole B200: a full load of warps for its 148 SMs)
+// Rows a warp looks at: one while that many warps still fit the GPU a few times over, up to 32 beyond.  Measured in a graph (us, with a
+// quarter of kAppendWarps, with it, with four times as many; 8 key heads of 128, pages of 64): 256 rows of tokens 4.8, 3.4 and 3.4, 1000
+// 14.0, 9.2 and 8.0, 3,700 rows of prompts 8.5, 9.5 and 13.1, 17,000 19.6, 19.6 and 24.1.  17,000 rows with up to 16 rows a warp 22, with
+// one (and more work a row) 73.  Loads of 16 bytes a lane that stay in registers: 8 there (20 us; 4: 21.4, 16: 20.5), 4 where a warp looks
+// at one row (256 rows: 3.5 us, with 16 7.7).
 template <typename T>
 static void append_launch(AppendArgs a, cudaStream_t s)
 {
@@ -156,6 +158,9 @@ static void attend_launch(AttendArgs a, const CUtensorMap& k, const CUtensorMap&
         g_launches = alike ? 3 : 5;
         if (alike) return;
     }
+    // the smallest tile of rows that has them all in one.  Measured (us, tiles of 8, 16 and 32 rows; 8 key heads of 128): 64 requests of
+    // 4096 to 8192 tokens, 8 rows a key head 138, 180 and 270, 16 rows 189 (16) and 276 (32); one request of 1000 tokens, 4 rows 9.8,
+    // 10.6 and 11.7
     const uint32_t workers = std::min(2u * sms, kMaxWorkers);
     if (rows <= 8) few_launch<T, D, 8>(a, k, v, workers, s);
     else if (rows <= 16) few_launch<T, D, 16>(a, k, v, workers, s);
@@ -181,6 +186,8 @@ wm_status wm_pages_plan(const int32_t* old_len, const int32_t* new_len, uint32_t
     const PlanArgs a = {old_len, new_len, n_requests, page_tokens, shift, n_pages, table, table_stride, free_pages, free_count,
                         free_count_out, start, slots, n_slots, n_slots > kPlanSlots, report};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    // one block, or a cluster of eight with a barrier among them.  Measured in a graph (us, one and eight): 64 requests 3.7 and 4.2, 1000
+    // 4.8 and 5.2, 2000 6.3 and 5.6, 4000 9.3 and 6.5 (a token each; 1024 requests with four each 6.8 and 5.0)
     const bool small = n_requests <= 1024u && n_slots <= kPlanSlots;
     launch_after_clustered(small ? k_pages_plan<false> : k_pages_plan<true>, small ? 1 : kPlanBlocks, kPlanThreads,
                            3u * (n_requests + 1u) * 4u, small ? 1 : kPlanBlocks, s, a);

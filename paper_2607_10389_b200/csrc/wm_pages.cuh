@@ -44,7 +44,9 @@ struct PlanArgs {
 constexpr uint32_t kPlanThreads = 1024;
 constexpr uint32_t kPlanPer = (kMaxRequests + kPlanThreads - 1) / kPlanThreads;    // requests a thread scans
 constexpr uint32_t kPlanBlocks = 8;                             // of a cluster
-constexpr uint32_t kPlanSlots = 4096;                           // slots up to which k_pages_plan lists them itself
+// Slots up to which k_pages_plan lists them itself.  Measured in a graph (us, there and in a kernel of their own): 256 requests with a
+// token each 4.0 and 6.6, 4000 6.5 and 10.2; 5,800 slots of 200 requests 8.2 and 6.6, 11,600 13.2 and 6.5.
+constexpr uint32_t kPlanSlots = 4096;
 
 // The last i with s[i] <= x (s ascending, s[0] = 0, s[n] > x).
 __device__ __forceinline__ uint32_t last_not_above(const uint32_t* s, uint32_t n, uint32_t x)
@@ -340,7 +342,7 @@ template <typename T> __device__ __forceinline__ void unpack8(const uint32_t (&w
 
 // A warp takes one run of rows that go into one page, for one head, keys or values: its largest value first, then the codes of
 // what the page keeps (only if the scale has grown), then the new rows'.  Bound by memory where runs are long (rows in once, codes
-// out once: 103 MB of prompts in 20 us, 0.79 of the copy rate), by the chain slot, row, scale, code where they are short (3.5 us).  A warp looks at `a.per_warp` rows for the firsts of runs,
+// out once: 103 MB of prompts in 20 us, 0.78 of the copy rate), by the chain slot, row, scale, code where they are short (3.5 us).  A warp looks at `a.per_warp` rows for the firsts of runs,
 // with a lane for each (one row a warp, prompts spent most of the call on starting warps that had nothing to do); a run of up to
 // kRows rows stays in registers between the two looks at it, of a longer one the last kRows do.
 // KL: loads in registers; few where a warp looks at one row and most runs are short (so that all warps fit at once), else as many as pay.

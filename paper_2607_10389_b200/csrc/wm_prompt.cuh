@@ -8,8 +8,8 @@ namespace wm {
 // A block takes 256 rows of one request and key head (rows run over the heads that share the key head first, then over the
 // queries), two tensor-core tiles of 128, and walks the tokens in tiles of 128:
 //   scores   S = Q K^T: e4m3 x e4m3.  The keys go in as they lie; a query is a sum of pieces (e4m3, then e5m2 for the
-//            remainders: 8 bits of a bf16 element in two pieces, 11 of an f16 in three, exact above 2^-17 and 2^-13 of the row's
-//            largest, else off by less than 2^-20 of it), so no key is ever converted, and two 8-bit passes cost what one
+//            remainders: 8 bits of a bf16 element in two pieces, 11 of an f16 in three, exact above 2^-13 of the row's
+//            largest, else off by 2^-21 of it at most), so no key is ever converted, and two 8-bit passes cost what one
 //            16-bit pass would.
 //   outputs  O += P V: f16 x f16 with the weights in tensor memory, over their scores.  Values are converted once per tile
 //            (exact) by a warpgroup of its own, for all 256 rows.
@@ -21,8 +21,8 @@ namespace wm {
 // other tile.
 // Work is dealt out as in the kernel for few rows: equal shares of tiles, units cut between workers are joined in order.
 //
-// Measured: four prompts' 1024 rows over 5000 to 9000 tokens (32 heads, 8 key heads of 128; 437 GFLOP) 393 us, 1.11 PFLOP/s, 0.68 of the
-// bf16 rate in short runs, 445 us in runs of seconds.  A pair of tiles takes 3400 cycles; the tensor cores need 2048 of them and the
+// Measured: four prompts' 1024 rows over 5000 to 9000 tokens (32 heads, 8 key heads of 128; 437 GFLOP) 394 us, 1.11 PFLOP/s, 0.68 of the
+// bf16 rate in short runs, 445 to 459 us in runs of seconds.  A pair of tiles takes 3400 cycles; the tensor cores need 2048 of them and the
 // exponentials 2130, but a tile's scores, softmax, weights and outputs follow one another, and only two tiles fit in tensor memory.
 
 // A worker's segments: consecutive tiles of one unit.  base, end: the first tile of its group's first key head, and behind its last's.
