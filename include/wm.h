@@ -523,9 +523,9 @@ wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows
  * kv_len[i] - n + j.  Query head h reads key head h / (q_heads / kv_heads).  A row at position p sees the request's tokens
  * t < kv_len[i], with causal only t <= p, with a window of w > 0 (causal only) only t > p - w.
  *   out = sum_t softmax_t(scale * q . key_t) value_t,   lse = log sum_t exp(scale * q . key_t)
- * A row that sees nothing (no tokens, or with causal a position below zero; without causal a row at such a position sees all tokens
- * as any other) gets zeros and -infinity.  Rows behind the last request's are
- * left as they are.  Codes a row does not see do not touch it, whatever they hold (NaN included).
+ * A row that sees nothing (no tokens, or with causal a position below zero; without causal a row at such a position sees all
+ * tokens as any other) gets zeros and -infinity.  Rows behind the last request's are left as they are.  Codes a row does not see
+ * do not touch it, whatever they hold (NaN included).
  *   table     [dev] i32[n_requests][table_stride], table_stride * page_tokens <= 2^30; kv_len [dev] i32[n_requests];
  *             q_start [dev] i32[n_requests + 1]
  *   q, out    n_rows rows of q_heads heads of the pool's head_dim, WM_TYPE_BF16 or WM_TYPE_F16; must not overlap, nor may
@@ -540,13 +540,14 @@ wm_status wm_pages_append(const wm_pages* pages, const wm_rows* k, const wm_rows
  *             calls (or captured graphs) that may run side by side need one each
  *   report    [dev] or NULL.  WM_ERR_ARG with the lowest request concerned: a negative length, a length beyond its row of
  *             the table, row numbers that decrease or lie outside 0 .. n_rows (its rows are left as they are), or
- *             a page number outside the pool (rows that see it get NaN).  WM_ERR_TIMEOUT: a wait ran out (see
+ *             a page number outside the pool (rows that see it get NaN; with a window, pages of up to 127 tokens in
+ *             front of what the rows see are looked up as well).  WM_ERR_TIMEOUT: a wait ran out (see
  *             wm_wait_budget_ms); outputs that are not there are NaN
  * Sums and softmax statistics are held in 32 bits.  The result of a row does not depend on the other requests' contents.
  * Queries are held as sums of 8-bit codes: exact for elements above 2^-13 of their row's and head's largest, else off by 2^-21 of
- * that at most (of 2^-119 where that is larger).  Weights have 11 bits or more; those far below the row's largest lie on a grid on which an output misses no
- * more than 2^-12 of the largest weight's share times the largest value, up to 2^25 tokens.  Outputs are summed by the tensor cores,
- * which lose products below 2^-25 of the sum that they are added to.
+ * that at most (of 2^-119 where that is larger).  Weights have 11 bits or more; those far below the row's largest lie on a grid on
+ * which an output misses no more than 2^-12 of the largest weight's share times the largest value, up to 2^25 tokens.  Outputs are
+ * summed by the tensor cores, which lose products below 2^-25 of the sum that they are added to.
  */
 #define WM_ATTEND_CAUSAL 1u
 uint64_t wm_pages_workspace_bytes(uint32_t head_dim);
